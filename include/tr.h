@@ -53,7 +53,8 @@
  * library prints nothing otherwise.  TR_ROCTX = 1 opens the roctx marker
  * library at the first call that enqueues work and brackets each call of
  * tr_reduce, tr_reduce_given_s, tr_reduce_project, tr_score, tr_select,
- * tr_gemm_bf16, tr_mlp_out_cos and tr_read_bandwidth in a range named after
+ * tr_gemm_bf16, tr_mlp_out_cos, tr_read_bandwidth, tr_kept_positions,
+ * tr_rotate, tr_rotate_backward, tr_append and tr_attend in a range named after
  * the entry point, so that a profiler's marker trace ties every call to its
  * kernels.  TR_FAIL_ALLOC and
  * TR_GEMM_TILE_ROWS are test hooks described at tr_create and tr_gemm_bf16.
@@ -342,6 +343,141 @@ tr_status tr_reduce_noalloc(const tr_params* p, const void* X, const void* X_pre
                             const int32_t* K, void* out, int32_t* out_idx,
                             uint8_t* out_src, float* out_h2, float* out_s,
                             void* stream);
+
+/* ---- The language model's side of the path (positions, heads, cache) -----
+ *
+ * What a model does with the kept tokens, from their indices to attention:
+ *   tr_kept_positions   (time, height, width) of each kept token
+ *   tr_rotate           norm of each query and key head, rotation by position
+ *   tr_rotate_backward  its gradients
+ *   tr_append           the same on the way of new keys into a paged cache
+ *   tr_attend           attention of the new tokens over that cache
+ *
+ * Rotation.  The first rot_dim elements of a head turn in pairs, pair i being
+ * elements (i, i + rot_dim / 2), or (2 i, 2 i + 1) with `adjacent`:
+ *   (a, b) -> (a cos z - b sin z, b cos z + a sin z),  z = pos[axis_i][t] freq_i.
+ * z is reduced to a fraction of a turn in 64-bit integers, so it is as exact at
+ * position 2^31 as at 1; sines and cosines are fp32.
+ * Norm (with `norm`): x_j -> x_j w_j / sqrt(sum_j x_j^2 / head_dim + eps) over a
+ * head, before its rotation; sums in fp32; a NULL weight is 1.
+ *
+ * Paged cache.  Token j of sequence b lies in page table[b][j / page_size], at
+ * row j % page_size of it.  The new tokens are packed back to back; sequence b's
+ * are q_start[b] .. q_start[b + 1] - 1 and are the last ones of its kv_len[b]
+ * tokens: the first of them is token kv_len[b] - (q_start[b + 1] - q_start[b]).
+ * Packed rows from q_start[seqs] on belong to no sequence: their outputs stay
+ * as they are.  q_start, kv_len and table are device memory, so a step recorded
+ * in a HIP graph replays with the lengths that they hold then.  They are not
+ * checked by the host: values out of range (a row outside [0, T), a length
+ * beyond table_width pages, a page outside [0, pages)) are never dereferenced;
+ * what they make of their sequence's rows is unspecified, except that tr_append
+ * writes no key or value for a token whose page is out of range. */
+typedef struct tr_attn tr_attn;
+
+typedef struct {
+    int32_t heads;        /* query heads (>= 1)                                    */
+    int32_t kv_heads;     /* key and value heads; divides heads                    */
+    int32_t head_dim;     /* elements of a head, 1 .. 256                          */
+    int32_t rot_dim;      /* leading elements that rotate: even, 0 .. head_dim     */
+    int32_t axes;         /* rows of pos, 1 .. 4                                   */
+    int32_t adjacent;     /* pairing, see above                                    */
+    int32_t dtype;        /* tr_dtype of every tensor of heads and of the weights  */
+    int32_t norm;         /* 1: heads are normed before they rotate                */
+    double eps;           /* of the norm (>= 0)                                    */
+    double base;          /* freq_i = base^(-2 i / rot_dim) where inv_freq is NULL  */
+    const double* inv_freq;    /* host [rot_dim / 2] finite angles per position, or NULL */
+    const int32_t* pair_axis;  /* host [rot_dim / 2] row of pos for each pair, or NULL: row 0 */
+} tr_attn_params;
+
+/* Heads of packed tokens: element j of head h of token t is at
+ * p + t * token + h * head + j (strides in elements). */
+typedef struct {
+    void* p;
+    int64_t token;
+    int64_t head;
+} tr_heads;
+
+/* A paged cache: element j of head h of row r of page g is at
+ * k (or v) + g * page + r * token + h * head + j. */
+typedef struct {
+    void* k;
+    void* v;
+    int32_t pages;
+    int32_t page_size;
+    int64_t page;
+    int64_t token;
+    int64_t head;
+} tr_cache;
+
+/* The sequences of one step (see above). */
+typedef struct {
+    int32_t seqs;
+    int32_t table_width;      /* pages in a row of table                            */
+    int64_t table_stride;     /* entries from one row of table to the next          */
+    const int32_t* q_start;   /* device [seqs + 1]                                  */
+    const int32_t* kv_len;    /* device [seqs], with the new tokens                 */
+    const int32_t* table;     /* device [seqs, table_width]                         */
+} tr_step;
+
+/* A layer's geometry on the current device, with the scratch of its calls
+ * (12 MB at head_dim 128): as with a tr_ctx, one stream at a time.  Errors as
+ * tr_create. */
+tr_status tr_attn_create(const tr_attn_params* p, tr_attn** out);
+void tr_attn_destroy(tr_attn* a);
+
+/* Positions of kept tokens: for image b of grid (T_b, H_b, W_b) and its kept
+ * token n at (t, h, w), n = (t H_b + h) W_b + w, column c of pos becomes
+ * start[b] + (t, h, w).  Images' columns are packed (dst NULL), or those of
+ * image b begin at column dst[b].
+ *   idx    device int32 [sum K], image-local (tr_reduce's out_idx)
+ *   K      host [B], >= 0 kept tokens of each image
+ *   grid   host [B, 3], each >= 1, and start host [B, 3]
+ *   dst    host [B] or NULL; image b's columns must end within ldpos
+ *   pos    device int32 [3, ldpos] (other columns stay as they are)
+ * Needs no context. */
+tr_status tr_kept_positions(const int32_t* idx, int32_t B, const int32_t* K, const int32_t* grid,
+                            const int32_t* start, const int64_t* dst, int32_t* pos, int64_t ldpos,
+                            void* stream);
+
+/* Norm and rotation of T tokens' heads: q [T, heads, head_dim] to q_out and
+ * k [T, kv_heads, head_dim] to k_out (which may be q and k themselves); a NULL
+ * q.p or k.p leaves that side out.  wq and wk: device [head_dim], or NULL
+ * (required NULL without `norm`).  pos: device int32 [axes, ldpos], ldpos >= T. */
+tr_status tr_rotate(tr_attn* a, int64_t T, tr_heads q, tr_heads k, const void* wq, const void* wk,
+                    const int32_t* pos, int64_t ldpos, tr_heads q_out, tr_heads k_out, void* stream);
+
+/* Gradients of tr_rotate: from gq and gk (of q_out and k_out) and the inputs q
+ * and k (not read without `norm`) to dq and dk, and with `norm` to the fp32 sums
+ * dwq and dwk [head_dim] over all tokens and heads (NULL: not wanted).  The sums
+ * are taken in one fixed order.  A side whose g.p is NULL is left out (its dw
+ * must then be NULL too).  dq and dk may be gq and gk themselves. */
+tr_status tr_rotate_backward(tr_attn* a, int64_t T, tr_heads gq, tr_heads gk, tr_heads q, tr_heads k,
+                             const void* wq, const void* wk, const int32_t* pos, int64_t ldpos,
+                             tr_heads dq, tr_heads dk, float* dwq, float* dwk, void* stream);
+
+/* tr_rotate for new tokens whose keys go to their place in the cache, their
+ * values (not normed, not rotated) beside them, and the queries to q_out (q.p
+ * NULL: keys and values alone). */
+tr_status tr_append(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, const void* wq,
+                    const void* wk, const int32_t* pos, int64_t ldpos, tr_heads q_out,
+                    const tr_cache* c, const tr_step* s, void* stream);
+
+/* Attention of the new tokens over the cache (bf16 contexts only): for new
+ * token i of sequence b (token p = kv_len[b] - n_b + i of it) and head h, with
+ * key head g = h / (heads / kv_heads),
+ *   out = sum_j softmax_j(scale q . k_j) v_j   over the tokens j it sees:
+ *   j <= p with `causal`, and of those j > p - window with window > 0 (window
+ *   needs causal); all kv_len[b] tokens otherwise.
+ * A row that sees no token, or whose scores are all -inf, is 0, its lse -inf.
+ * Scores and sums are fp32; the weights are rounded to bf16 for their product
+ * with v.  Elements that a row does not see do not change it, NaN and infinite
+ * ones included.
+ *   lse: device float [T, heads] natural logarithm of the softmax's sum, or NULL
+ * head_dim must be a multiple of 8, and q's, out's and the cache's bases and
+ * strides of 16 bytes, else TR_EUNSUPPORTED. */
+tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const tr_step* s,
+                    double scale, int32_t causal, int32_t window, tr_heads out, float* lse,
+                    void* stream);
 
 /* Release the context and its scratch (NULL is a no-op).  Freeing device
  * memory waits for the device to finish outstanding work first. */

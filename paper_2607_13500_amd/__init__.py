@@ -8,6 +8,9 @@ Every step of the path runs in the HIP library libaltr.so (gfx950):
            the cosine, stride picks, union in token order (LDS-resident);
 * gather - byte copies of the kept rows into a compact [sum K, D] output.
 
+What a language model then does with the kept tokens (positions, rotated heads,
+a paged cache, attention over it) is in attention.py.
+
 This module only marshals torch tensors (device memory) and the current torch
 stream into the C ABI; it computes nothing itself.  If the library is missing
 or the tensors are not on a ROCm device, calls raise.
@@ -21,8 +24,10 @@ import torch
 
 from . import _lib
 from ._lib import Params
+from .attention import Attention, KVCache, Step, kept_positions
 
-__all__ = ["Reducer", "ReduceResult", "TRError", "plan", "capacity_N", "reduce_noalloc", "LAMBDA_PAPER"]
+__all__ = ["Reducer", "ReduceResult", "TRError", "plan", "capacity_N", "reduce_noalloc", "LAMBDA_PAPER",
+           "Attention", "KVCache", "Step", "kept_positions"]
 
 LAMBDA_PAPER = 1.0 / 3.0   # 64 importance + 128 diversity of 192 (efficiency setting)
 

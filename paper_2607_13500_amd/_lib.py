@@ -31,6 +31,54 @@ class Params(ctypes.Structure):
     ]
 
 
+class AttnParams(ctypes.Structure):
+    """Mirror of tr_attn_params in include/tr.h."""
+    _fields_ = [
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("axes", ctypes.c_int32),
+        ("adjacent", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("norm", ctypes.c_int32),
+        ("eps", ctypes.c_double),
+        ("base", ctypes.c_double),
+        ("inv_freq", ctypes.c_void_p),
+        ("pair_axis", ctypes.c_void_p),
+    ]
+
+
+class Heads(ctypes.Structure):
+    """Mirror of tr_heads in include/tr.h."""
+    _fields_ = [("p", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class Cache(ctypes.Structure):
+    """Mirror of tr_cache in include/tr.h."""
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("page", ctypes.c_int64),
+        ("token", ctypes.c_int64),
+        ("head", ctypes.c_int64),
+    ]
+
+
+class StepArgs(ctypes.Structure):
+    """Mirror of tr_step in include/tr.h."""
+    _fields_ = [
+        ("seqs", ctypes.c_int32),
+        ("table_width", ctypes.c_int32),
+        ("table_stride", ctypes.c_int64),
+        ("q_start", ctypes.c_void_p),
+        ("kv_len", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+    ]
+
+
 TR_OK, TR_EINVAL, TR_ENOMEM, TR_EUNSUPPORTED, TR_EDEVICE = range(5)
 TR_FP32, TR_BF16 = 0, 1
 TR_FLAG_STRIDE_REAL = 1
@@ -88,6 +136,21 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.tr_timing_read.restype = i32
     lib.tr_destroy.argtypes = [vp]
     lib.tr_destroy.restype = None
+    H = Heads
+    lib.tr_attn_create.argtypes = [P(AttnParams), P(vp)]
+    lib.tr_attn_create.restype = i32
+    lib.tr_attn_destroy.argtypes = [vp]
+    lib.tr_attn_destroy.restype = None
+    lib.tr_kept_positions.argtypes = [vp, i32, vp, vp, vp, vp, vp, i64, vp]
+    lib.tr_kept_positions.restype = i32
+    lib.tr_rotate.argtypes = [vp, i64, H, H, vp, vp, vp, i64, H, H, vp]
+    lib.tr_rotate.restype = i32
+    lib.tr_rotate_backward.argtypes = [vp, i64, H, H, H, H, vp, vp, vp, i64, H, H, vp, vp, vp]
+    lib.tr_rotate_backward.restype = i32
+    lib.tr_append.argtypes = [vp, i64, H, H, H, vp, vp, vp, i64, H, P(Cache), P(StepArgs), vp]
+    lib.tr_append.restype = i32
+    lib.tr_attend.argtypes = [vp, i64, H, P(Cache), P(StepArgs), ctypes.c_double, i32, i32, H, vp, vp]
+    lib.tr_attend.restype = i32
     lib.tr_strerror.argtypes = [i32]
     lib.tr_strerror.restype = ctypes.c_char_p
     lib.tr_last_error.argtypes = []
