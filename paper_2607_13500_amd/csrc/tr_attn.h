@@ -47,7 +47,7 @@ struct RotateArgs {
     const void* w[2];          // norm weights of queries and keys, or nullptr: 1
     const int32_t* pos;        // [axes, ldpos]
     int64_t ldpos;
-    const uint64_t* turn;      // [rot / 2] turns per position, as fractions of 2^64
+    const float* freq;         // [rot / 2] angle per position
     const int32_t* pair_axis;  // [rot / 2]
     float* part;               // backward: partial sums of dw
     float* dw[2];              // backward: sums, or nullptr

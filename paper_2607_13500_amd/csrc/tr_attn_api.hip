@@ -26,7 +26,7 @@ struct tr_attn {
     int device = 0;
     int eb = 4;
     int cus = 256;
-    uint64_t* turn = nullptr;       // [rot_dim / 2], see RotateArgs
+    float* freq = nullptr;          // [rot_dim / 2], see RotateArgs
     int32_t* pair_axis = nullptr;   // [rot_dim / 2]
     float* part = nullptr;          // partial sums of dw
 };
@@ -60,15 +60,6 @@ tr_status check_attn_params(const tr_attn_params* p)
             return fail(TR_EINVAL, "pair_axis[%d] = %d must be in [0, %d)", i, p->pair_axis[i], p->axes);
     }
     return TR_OK;
-}
-
-// The fraction of a turn that an angle of x radians is, in units of 2^-64.
-uint64_t turns_of(long double x)
-{
-    const long double turns = x / (2.0L * 3.14159265358979323846264338327950288L);
-    long double f = turns - floorl(turns);             // [0, 1]
-    f = roundl(f * 18446744073709551616.0L);           // 2^64
-    return f >= 18446744073709551616.0L ? 0u : (uint64_t)f;
 }
 
 // Whether rows of dim elements at the given strides (each with its count)
@@ -170,7 +161,7 @@ tr::RotateArgs rotate_args(const tr_attn* a, int64_t T, const void* wq, const vo
     r.w[1] = wk;
     r.pos = pos;
     r.ldpos = ldpos;
-    r.turn = a->turn;
+    r.freq = a->freq;
     r.pair_axis = a->pair_axis;
     r.part = a->part;
     r.cus = a->cus;
@@ -188,12 +179,11 @@ tr_status tr_attn_create(const tr_attn_params* p, tr_attn** out)
     *out = nullptr;
     tr_status st = check_attn_params(p);
     if (st != TR_OK) return st;
-    uint64_t turn[tr::kMaxHeadDim / 2] = {};
+    float freq[tr::kMaxHeadDim / 2] = {};
     int32_t axis[tr::kMaxHeadDim / 2] = {};
     const int pairs = p->rot_dim / 2;
     for (int i = 0; i < pairs; ++i) {
-        turn[i] = turns_of(p->inv_freq ? (long double)p->inv_freq[i]
-                                       : powl((long double)p->base, -(long double)(2 * i) / (long double)p->rot_dim));
+        freq[i] = (float)(p->inv_freq ? p->inv_freq[i] : pow(p->base, -(double)(2 * i) / (double)p->rot_dim));
         axis[i] = p->pair_axis ? p->pair_axis[i] : 0;
     }
     int dev = 0;
@@ -211,12 +201,12 @@ tr_status tr_attn_create(const tr_attn_params* p, tr_attn** out)
         return hip_fail(e, "hipDeviceGetAttribute");
     }
     CtxAlloc al;
-    if ((e = al(&a->turn, sizeof turn)) != hipSuccess || (e = al(&a->pair_axis, sizeof axis)) != hipSuccess ||
+    if ((e = al(&a->freq, sizeof freq)) != hipSuccess || (e = al(&a->pair_axis, sizeof axis)) != hipSuccess ||
         (e = al(&a->part, tr::rotate_part_floats(p->head_dim, a->cus) * sizeof(float))) != hipSuccess) {
         tr_attn_destroy(a);
         return fail(TR_ENOMEM, "hipMalloc of a layer's scratch failed: %s", hipGetErrorString(e));
     }
-    if ((e = hipMemcpy(a->turn, turn, sizeof turn, hipMemcpyHostToDevice)) != hipSuccess ||
+    if ((e = hipMemcpy(a->freq, freq, sizeof freq, hipMemcpyHostToDevice)) != hipSuccess ||
         (e = hipMemcpy(a->pair_axis, axis, sizeof axis, hipMemcpyHostToDevice)) != hipSuccess ||
         (e = hipDeviceSynchronize()) != hipSuccess) {
         tr_attn_destroy(a);
@@ -233,7 +223,7 @@ void tr_attn_destroy(tr_attn* a)
 {
     if (!a) return;
     DeviceGuard g(a->device);
-    if (a->turn) (void)hipFree(a->turn);
+    if (a->freq) (void)hipFree(a->freq);
     if (a->pair_axis) (void)hipFree(a->pair_axis);
     if (a->part) (void)hipFree(a->part);
     delete a;

@@ -4,13 +4,13 @@
 // gradient  dx = r (gw - u mean(gw u)),  dw = sum g u,  with g = R^T dy,
 // r = 1 / sqrt(mean x^2 + eps), u = x r, gw = g w.
 //
-// Angles.  A frequency is kept as the fraction of a turn per position in 64
-// bits; the product with the position, modulo 2^64, is the exact fraction of
-// that frequency's turn at any int32 position.  Its upper 32 bits give the
-// quarter and a rest of at most an eighth of a turn, where the Taylor series of
+// Angles are formed as models form them, as the fp32 product of a position and a
+// frequency.  That angle's fraction of a turn is taken in fp64, split into the
+// nearest quarter and a rest of at most an eighth, where the Taylor series of
 // sine and cosine to x^9 and x^10 are below 2e-9 off.
 //
 // All of it is bound by memory: heads are read once and written once.
+#include <algorithm>
 #include <type_traits>
 
 #include "tr_attn.h"
@@ -42,13 +42,15 @@ struct Turn {
     float c, s;
 };
 
-// Cosine and sine of pos * turn / 2^64 of a turn.
-__device__ __forceinline__ Turn turn_of(int32_t pos, uint64_t turn)
+// Cosine and sine of the fp32 angle pos * freq.
+__device__ __forceinline__ Turn turn_of(int32_t pos, float freq)
 {
-    const uint64_t z = (uint64_t)(int64_t)pos * turn;
-    const uint32_t f = (uint32_t)(z >> 32);
-    const uint32_t quarter = (f + 0x20000000u) >> 30;
-    const float x = (float)(int32_t)(f - (quarter << 30)) * 0x1.921fb6p-30f;   // 2 pi / 2^32
+    const float angle = (float)pos * freq;
+    double z = (double)angle * 0.15915494309189535;   // 1 / 2 pi
+    z = (z - rint(z)) * 4.0;                          // quarters, [-2, 2]
+    const double near = rint(z);
+    const float x = (float)(z - near) * 1.57079632679f;
+    const int quarter = (int)near;
     const float x2 = x * x;
     float s = fmaf(x2, 2.75573192e-6f, -1.98412698e-4f);
     s = fmaf(x2, s, 8.33333333e-3f);
@@ -59,11 +61,11 @@ __device__ __forceinline__ Turn turn_of(int32_t pos, uint64_t turn)
     c = fmaf(x2, c, 4.16666667e-2f);
     c = fmaf(x2, c, -0.5f);
     c = fmaf(x2, c, 1.f);
-    const bool odd = quarter & 1u;
+    const bool odd = quarter & 1;
     const float cc = odd ? s : c, ss = odd ? c : s;
     Turn r;
-    r.c = (quarter + 1u) & 2u ? -cc : cc;   // quarters 1 and 2
-    r.s = quarter & 2u ? -ss : ss;          // quarters 2 and 3
+    r.c = (quarter + 1) & 2 ? -cc : cc;   // quarters 1 and 2
+    r.s = quarter & 2 ? -ss : ss;         // quarters 2 and 3
     return r;
 }
 
@@ -191,7 +193,7 @@ struct AnyHead {
         for (int j = 0; j < kPairs; ++j) {
             const int i = lane + 64 * j;
             if (i < g.rot / 2) {
-                const Turn z = turn_of(g.pos[(int64_t)g.pair_axis[i] * g.ldpos + t], g.turn[i]);
+                const Turn z = turn_of(g.pos[(int64_t)g.pair_axis[i] * g.ldpos + t], g.freq[i]);
                 const float s = back ? -z.s : z.s, x = a[j], y = b[j];
                 a[j] = fmaf(x, z.c, -(y * s));
                 b[j] = fmaf(y, z.c, x * s);
@@ -279,34 +281,443 @@ __global__ __launch_bounds__(256) void rotate_back_any_kernel(RotateArgs g)
         g.part[((int64_t)kind * gridDim.x + blockIdx.x) * g.dim + j] = (red[0][j] + red[1][j]) + (red[2][j] + red[3][j]);
 }
 
-// dw[kind][j] = sum over the workgroups' rows, in order: one wavefront an element.
-__global__ __launch_bounds__(64) void sum_parts_kernel(RotateArgs g, int parts)
+// dw[kind][j] = sum over the workgroups' rows of `part`: 32 columns to a
+// workgroup, 32 threads to a column, joined in a fixed order.
+__global__ __launch_bounds__(1024) void sum_parts_kernel(RotateArgs g, int parts)
 {
-    const int kind = blockIdx.y, j = blockIdx.x;
-    if (!g.dw[kind]) return;
+    __shared__ float red[32][33];
+    const int kind = blockIdx.y, col = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int j = blockIdx.x * 32 + col;
+    if (!g.dw[kind]) return;   // the whole workgroup leaves together
     float s = 0.f;
-    for (int i = threadIdx.x; i < parts; i += 64) s += g.part[((int64_t)kind * parts + i) * g.dim + j];
-    s = sum64(s);
-    if (threadIdx.x == 0) g.dw[kind][j] = s;
+    if (j < g.dim)
+        for (int i = row; i < parts; i += 32) s += g.part[((int64_t)kind * parts + i) * g.dim + j];
+    red[row][col] = s;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v += red[i][col];
+        if (j < g.dim) g.dw[kind][j] = v;
+    }
 }
 
+// ---- heads of whole 16-byte pieces: LP lanes a head --------------------------------
+// Lane j of the LP that share a head holds two 16-byte pieces of it: the first
+// and the second elements of C pairs (or, where pairs are adjacent, C pairs one
+// after another), and past the rotated part any two pieces.  All the lanes of a
+// group keep their sines and cosines while the wavefront walks over a token's
+// heads, 64 / LP at a time.
+template <typename E>
+struct Piece {
+    static constexpr int C = 16 / (int)sizeof(E);
+    float a[C], b[C];   // of pair i: a[i], b[i]; past the rotated part: the two pieces
+};
+
+template <typename E, bool ADJ>
+__device__ __forceinline__ Piece<E> unpack(u32x4 x, u32x4 y)
+{
+    constexpr int C = Piece<E>::C;
+    Piece<E> p;
+    float v[2 * C];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w0 = x[i], w1 = y[i];
+        if constexpr (C == 8) {
+            v[2 * i] = __uint_as_float(w0 << 16);
+            v[2 * i + 1] = __uint_as_float(w0 & 0xffff0000u);
+            v[C + 2 * i] = __uint_as_float(w1 << 16);
+            v[C + 2 * i + 1] = __uint_as_float(w1 & 0xffff0000u);
+        } else {
+            v[i] = __uint_as_float(w0);
+            v[C + i] = __uint_as_float(w1);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        p.a[i] = ADJ ? v[2 * i] : v[i];
+        p.b[i] = ADJ ? v[2 * i + 1] : v[C + i];
+    }
+    return p;
+}
+
+template <typename E, bool ADJ>
+__device__ __forceinline__ void pack(const Piece<E>& p, u32x4& x, u32x4& y)
+{
+    constexpr int C = Piece<E>::C;
+    float v[2 * C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        v[ADJ ? 2 * i : i] = p.a[i];
+        v[ADJ ? 2 * i + 1 : C + i] = p.b[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (C == 8) {
+            x[i] = (uint32_t)narrow<E>(v[2 * i]) | (uint32_t)narrow<E>(v[2 * i + 1]) << 16;
+            y[i] = (uint32_t)narrow<E>(v[C + 2 * i]) | (uint32_t)narrow<E>(v[C + 2 * i + 1]) << 16;
+        } else {
+            x[i] = __float_as_uint(v[i]);
+            y[i] = __float_as_uint(v[C + i]);
+        }
+    }
+}
+
+// Sum over each group of LP lanes, the same bits in all of them.
+template <int LP>
+__device__ __forceinline__ float group_sum(float x)
+{
+#pragma unroll
+    for (int m = 1; m < LP; m <<= 1) x += __shfl_xor(x, m);
+    return x;
+}
+
+// Where lane j's two pieces begin in a head, and whether they rotate.
+struct Spot {
+    int e0, e1;
+    bool on, turns;
+};
+
+template <int C, bool ADJ>
+__device__ __forceinline__ Spot spot_of(int j, int dim, int rot)
+{
+    Spot s;
+    s.on = j < dim / (2 * C);
+    s.turns = j < rot / (2 * C);
+    s.e0 = s.turns && !ADJ ? C * j : 2 * C * j;
+    s.e1 = s.turns && !ADJ ? rot / 2 + C * j : 2 * C * j + C;
+    return s;
+}
+
+// What lane j's C pairs turn by: their frequencies, and two bits of axis each.
+template <int C>
+struct Spin {
+    float freq[C];
+    uint32_t axes;
+};
+
+template <int C>
+__device__ __forceinline__ Spin<C> spin_of(const RotateArgs& g, int j, bool turns)
+{
+    Spin<C> s;
+    s.axes = 0;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        s.freq[i] = turns ? g.freq[C * j + i] : 0.f;
+        s.axes |= turns ? (uint32_t)g.pair_axis[C * j + i] << (2 * i) : 0u;
+    }
+    return s;
+}
+
+// The C turns of a lane for token t (none: cosine 1, sine 0).
+template <int C>
+__device__ __forceinline__ void turns_of(const RotateArgs& g, const Spin<C>& spin, int64_t t, float (&c)[C], float (&s)[C])
+{
+    static_assert(kMaxAxes == 4, "an axis is two bits");
+    int32_t at[kMaxAxes];
+#pragma unroll
+    for (int x = 0; x < kMaxAxes; ++x) at[x] = x < g.axes && g.rot ? g.pos[(int64_t)x * g.ldpos + t] : 0;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int32_t lo = spin.axes >> (2 * i) & 1u ? at[1] : at[0], hi = spin.axes >> (2 * i) & 1u ? at[3] : at[2];
+        const Turn z = turn_of(spin.axes >> (2 * i) & 2u ? hi : lo, spin.freq[i]);
+        c[i] = z.c;
+        s[i] = z.s;
+        __builtin_amdgcn_sched_barrier(0);   // one at a time: side by side they take twice the registers
+    }
+}
+
+template <typename E, bool ADJ>
+__device__ __forceinline__ Piece<E> load_weight(const void* w, const Spot& sp)
+{
+    Piece<E> p;
+    if (w && sp.on) {
+        const E* q = static_cast<const E*>(w);
+        return unpack<E, ADJ>(*reinterpret_cast<const u32x4*>(q + sp.e0), *reinterpret_cast<const u32x4*>(q + sp.e1));
+    }
+#pragma unroll
+    for (int i = 0; i < Piece<E>::C; ++i) p.a[i] = p.b[i] = 1.f;
+    return p;
+}
+
+// A wavefront takes `per` rounds of 64 / LP heads of one token.
+template <typename E, int LP, bool ADJ, bool APPEND>
+__global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int chunks)
+{
+    constexpr int C = Piece<E>::C, R = 64 / LP;
+    const int lane = threadIdx.x & 63, j = lane & (LP - 1);
+    const int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t = u / chunks;
+    if (t >= g.tokens) return;
+    const int rows = g.heads[0] + g.heads[1] + g.heads[2];
+    const int first = (int)(u - t * chunks) * per * R + lane / LP;
+    const Spot sp = spot_of<C, ADJ>(j, g.dim, g.rot);
+
+    // the head of row r: its side, and where it lies
+    auto source = [&](int r, int& kind) -> const E* {
+        int h = r;
+        kind = 0;
+        if (h >= g.heads[0]) {
+            h -= g.heads[0];
+            kind = 1;
+            if (APPEND && h >= g.heads[1]) {
+                h -= g.heads[1];
+                kind = 2;
+            }
+        }
+        const tr_heads& in = g.in[kind];
+        return static_cast<const E*>(in.p) + t * in.token + (int64_t)h * in.head;
+    };
+    u32x4 n0{}, n1{};
+    int kind_n = 0;
+    auto fetch = [&](int r) {
+        if (r < rows && sp.on) {
+            const E* p = source(r, kind_n);
+            n0 = *reinterpret_cast<const u32x4*>(p + sp.e0);
+            n1 = *reinterpret_cast<const u32x4*>(p + sp.e1);
+        }
+    };
+    fetch(first);
+    int64_t row = 0;
+    if constexpr (APPEND) {
+        row = cache_row(g.step, g.cache, t, lane);
+        if (row == kNoToken) return;
+    }
+    float c[C], s[C];
+    turns_of<C>(g, spin_of<C>(g, j, sp.turns), t, c, s);
+    Piece<E> wq, wk;
+    if (g.norm) {
+        wq = load_weight<E, ADJ>(g.w[0], sp);
+        wk = load_weight<E, ADJ>(g.w[1], sp);
+    }
+    for (int i = 0; i < per; ++i) {
+        const int r = first + i * R;
+        if (__builtin_amdgcn_readfirstlane(r) >= rows) break;     // lane 0 holds the wavefront's first head
+        u32x4 x0 = n0, x1 = n1;
+        const int kind = kind_n;
+        if (i + 1 < per) fetch(r + R);
+        if (!APPEND || kind < 2) {
+            Piece<E> x = unpack<E, ADJ>(x0, x1);
+            if (g.norm) {
+                float q = 0.f;
+#pragma unroll
+                for (int e = 0; e < C; ++e) q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
+                q = group_sum<LP>(sp.on ? q : 0.f);
+                const float m = 1.f / sqrtf(q / (float)g.dim + g.eps);
+#pragma unroll
+                for (int e = 0; e < C; ++e) {
+                    x.a[e] = x.a[e] * m * (kind ? wk.a[e] : wq.a[e]);
+                    x.b[e] = x.b[e] * m * (kind ? wk.b[e] : wq.b[e]);
+                }
+            }
+            Piece<E> y = x;
+            if (sp.turns) {
+#pragma unroll
+                for (int e = 0; e < C; ++e) {
+                    y.a[e] = fmaf(x.a[e], c[e], -(x.b[e] * s[e]));
+                    y.b[e] = fmaf(x.b[e], c[e], x.a[e] * s[e]);
+                }
+            }
+            pack<E, ADJ>(y, x0, x1);
+        }
+        if (r < rows && sp.on) {
+            const int h = r - (kind > 0 ? g.heads[0] : 0) - (kind > 1 ? g.heads[1] : 0);
+            E* p;
+            if (APPEND && kind > 0) {
+                if (row == kNoRow) continue;
+                p = static_cast<E*>(kind == 1 ? g.cache.k : g.cache.v) + row + (int64_t)h * g.cache.head;
+            } else {
+                p = static_cast<E*>(g.out[kind].p) + t * g.out[kind].token + (int64_t)h * g.out[kind].head;
+            }
+            *reinterpret_cast<u32x4*>(p + sp.e0) = x0;
+            *reinterpret_cast<u32x4*>(p + sp.e1) = x1;
+        }
+    }
+}
+
+// Gradients of one side (blockIdx.y): a wavefront walks over tokens t, t +
+// waves, ... and their heads, and keeps its lanes' share of dw, which a
+// workgroup joins into its row of `part`.
+template <typename E, int LP, bool ADJ>
+__global__ __launch_bounds__(256, 4) void rotate_back_kernel(RotateArgs g)
+{
+    constexpr int C = Piece<E>::C, R = 64 / LP;
+    __shared__ float red[4][kMaxHeadDim];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane & (LP - 1), kind = blockIdx.y;
+    const int rows = g.heads[kind];
+    const int64_t waves = (int64_t)gridDim.x * 4;
+    const Spot sp = spot_of<C, ADJ>(j, g.dim, g.rot);
+    const tr_heads hg = g.grad[kind], hx = g.in[kind], ho = g.out[kind];
+    const Spin<C> spin = spin_of<C>(g, j, sp.turns);
+    Piece<E> w, dw;
+    if (g.norm) w = load_weight<E, ADJ>(g.w[kind], sp);
+#pragma unroll
+    for (int e = 0; e < C; ++e) dw.a[e] = dw.b[e] = 0.f;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(wave); t < g.tokens; t += waves) {
+        u32x4 g0{}, g1{}, x0{}, x1{};
+        auto fetch = [&](int r) {
+            if (r < rows && sp.on) {
+                const E* p = static_cast<const E*>(hg.p) + t * hg.token + (int64_t)r * hg.head;
+                g0 = *reinterpret_cast<const u32x4*>(p + sp.e0);
+                g1 = *reinterpret_cast<const u32x4*>(p + sp.e1);
+                if (g.norm) {
+                    const E* q = static_cast<const E*>(hx.p) + t * hx.token + (int64_t)r * hx.head;
+                    x0 = *reinterpret_cast<const u32x4*>(q + sp.e0);
+                    x1 = *reinterpret_cast<const u32x4*>(q + sp.e1);
+                }
+            }
+        };
+        fetch(lane / LP);
+        float c[C], s[C];
+        turns_of<C>(g, spin, t, c, s);
+        for (int r = lane / LP; __builtin_amdgcn_readfirstlane(r) < rows; r += R) {
+            const bool live = r < rows && sp.on;
+            const Piece<E> d = unpack<E, ADJ>(g0, g1);
+            Piece<E> x;
+            if (g.norm) x = unpack<E, ADJ>(x0, x1);
+            fetch(r + R);
+            Piece<E> y = d;
+            if (sp.turns) {
+#pragma unroll
+                for (int e = 0; e < C; ++e) {
+                    y.a[e] = fmaf(d.a[e], c[e], d.b[e] * s[e]);
+                    y.b[e] = fmaf(d.b[e], c[e], -(d.a[e] * s[e]));
+                }
+            }
+            if (g.norm) {
+                float q = 0.f, m = 0.f;
+#pragma unroll
+                for (int e = 0; e < C; ++e) {
+                    q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
+                    m = fmaf(y.a[e] * w.a[e], x.a[e], fmaf(y.b[e] * w.b[e], x.b[e], m));
+                }
+                q = group_sum<LP>(live ? q : 0.f);
+                m = group_sum<LP>(live ? m : 0.f);
+                const float n = 1.f / sqrtf(q / (float)g.dim + g.eps);
+                m = m * n / (float)g.dim;
+#pragma unroll
+                for (int e = 0; e < C; ++e) {
+                    const float ua = x.a[e] * n, ub = x.b[e] * n;
+                    dw.a[e] += live ? y.a[e] * ua : 0.f;
+                    dw.b[e] += live ? y.b[e] * ub : 0.f;
+                    y.a[e] = n * fmaf(-ua, m, y.a[e] * w.a[e]);
+                    y.b[e] = n * fmaf(-ub, m, y.b[e] * w.b[e]);
+                }
+            }
+            if (live) {
+                u32x4 y0, y1;
+                pack<E, ADJ>(y, y0, y1);
+                E* p = static_cast<E*>(ho.p) + t * ho.token + (int64_t)r * ho.head;
+                *reinterpret_cast<u32x4*>(p + sp.e0) = y0;
+                *reinterpret_cast<u32x4*>(p + sp.e1) = y1;
+            }
+        }
+    }
+    if (!g.dw[kind]) return;   // the whole workgroup leaves together
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+        float a = dw.a[e], b = dw.b[e];
+#pragma unroll
+        for (int m = LP; m < 64; m <<= 1) {
+            a += __shfl_xor(a, m);
+            b += __shfl_xor(b, m);
+        }
+        if (lane < LP && sp.on) {
+            red[wave][ADJ ? sp.e0 + 2 * e : sp.e0 + e] = a;
+            red[wave][ADJ ? sp.e0 + 2 * e + 1 : sp.e1 + e] = b;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < g.dim; i += 256)
+        g.part[((int64_t)kind * gridDim.x + blockIdx.x) * g.dim + i] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+}
+
+// ---- launches ------------------------------------------------------------------------
 int back_groups(int cus) { return 4 * cus; }
 
-template <typename E>
-hipError_t rotate_any(const RotateArgs& a, hipStream_t s)
+bool whole(const tr_heads& h, int eb)
 {
-    const int64_t rows = a.tokens * (a.heads[0] + a.heads[1] + a.heads[2]);
-    hipLaunchKernelGGL(rotate_any_kernel<E>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return ((uintptr_t)h.p | (uintptr_t)(h.token * eb) | (uintptr_t)(h.head * eb)) % 16 == 0;
+}
+
+// Whether every head of the call is made of whole 16-byte pieces: its address,
+// its halves and its rotated part.
+bool in_pieces(const RotateArgs& a, int eb, bool back)
+{
+    const int two = 32 / eb;
+    if (a.dim % two || a.rot % two) return false;
+    for (int k = 0; k < 3; ++k) {
+        if (!a.heads[k]) continue;
+        const bool to_cache = a.append && k > 0;
+        if (!whole(a.in[k], eb) && !(back && !a.norm)) return false;
+        if (!to_cache && !whole(a.out[k], eb)) return false;
+        if (back && !whole(a.grad[k], eb)) return false;
+        if (k < 2 && (uintptr_t)a.w[k] % 16) return false;
+    }
+    return !a.append || ((((uintptr_t)a.cache.k | (uintptr_t)a.cache.v) % 16 == 0) &&
+                         ((a.cache.page | a.cache.token | a.cache.head) * eb) % 16 == 0);
+}
+
+template <typename E, int LP>
+hipError_t rotate_pieces(const RotateArgs& a, hipStream_t s)
+{
+    const int rows = a.heads[0] + a.heads[1] + a.heads[2];
+    const int rounds = (rows * LP + 63) / 64;
+    // All of a token's heads to a wavefront, which then works its angles out once,
+    // where that leaves the chip full; else a round each.
+    const int per = a.tokens >= 16 * (int64_t)a.cus ? rounds : 1;
+    const int chunks = (rounds + per - 1) / per;
+    const int64_t groups = (a.tokens * chunks + 3) / 4;
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, s, a, per, chunks);
+        return hipGetLastError();
+    };
+    if (a.append) return a.adjacent ? launch(rotate_kernel<E, LP, true, true>) : launch(rotate_kernel<E, LP, false, true>);
+    return a.adjacent ? launch(rotate_kernel<E, LP, true, false>) : launch(rotate_kernel<E, LP, false, false>);
+}
+
+template <typename E, int LP>
+hipError_t back_pieces(const RotateArgs& a, int groups, hipStream_t s)
+{
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups, 2), dim3(256), 0, s, a);
+        return hipGetLastError();
+    };
+    return a.adjacent ? launch(rotate_back_kernel<E, LP, true>) : launch(rotate_back_kernel<E, LP, false>);
 }
 
 template <typename E>
-hipError_t back_any(const RotateArgs& a, hipStream_t s)
+hipError_t rotate_typed(const RotateArgs& a, hipStream_t s)
 {
-    hipLaunchKernelGGL(rotate_back_any_kernel<E>, dim3((unsigned)back_groups(a.cus), 2), dim3(256), 0, s, a);
-    hipError_t e = hipGetLastError();
+    if (!in_pieces(a, (int)sizeof(E), false)) {
+        const int64_t rows = a.tokens * (a.heads[0] + a.heads[1] + a.heads[2]);
+        hipLaunchKernelGGL(rotate_any_kernel<E>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
+    const int lanes = a.dim * (int)sizeof(E) / 32;
+    if (lanes <= 4) return rotate_pieces<E, 4>(a, s);
+    if (lanes <= 8) return rotate_pieces<E, 8>(a, s);
+    if (lanes <= 16) return rotate_pieces<E, 16>(a, s);
+    return rotate_pieces<E, 32>(a, s);
+}
+
+template <typename E>
+hipError_t back_typed(const RotateArgs& a, hipStream_t s)
+{
+    const bool pieces = in_pieces(a, (int)sizeof(E), true);
+    const int64_t units = pieces ? a.tokens : a.tokens * (a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1]);
+    const int groups = (int)std::max((int64_t)1, std::min((int64_t)back_groups(a.cus), (units + 3) / 4));
+    hipError_t e;
+    if (!pieces) {
+        hipLaunchKernelGGL(rotate_back_any_kernel<E>, dim3((unsigned)groups, 2), dim3(256), 0, s, a);
+        e = hipGetLastError();
+    } else {
+        const int lanes = a.dim * (int)sizeof(E) / 32;
+        e = lanes <= 4 ? back_pieces<E, 4>(a, groups, s) : lanes <= 8 ? back_pieces<E, 8>(a, groups, s)
+            : lanes <= 16 ? back_pieces<E, 16>(a, groups, s) : back_pieces<E, 32>(a, groups, s);
+    }
     if (e == hipSuccess && (a.dw[0] || a.dw[1])) {
-        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)a.dim, 2), dim3(64), 0, s, a, back_groups(a.cus));
+        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)(a.dim + 31) / 32, 2), dim3(1024), 0, s, a, groups);
         e = hipGetLastError();
     }
     return e;
@@ -325,12 +736,12 @@ size_t rotate_part_floats(int dim, int cus) { return (size_t)2 * back_groups(cus
 
 hipError_t launch_rotate(const RotateArgs& a, bool bf16, hipStream_t s)
 {
-    return bf16 ? rotate_any<uint16_t>(a, s) : rotate_any<float>(a, s);
+    return bf16 ? rotate_typed<uint16_t>(a, s) : rotate_typed<float>(a, s);
 }
 
 hipError_t launch_rotate_backward(const RotateArgs& a, bool bf16, hipStream_t s)
 {
-    return bf16 ? back_any<uint16_t>(a, s) : back_any<float>(a, s);
+    return bf16 ? back_typed<uint16_t>(a, s) : back_typed<float>(a, s);
 }
 
 }  // namespace tr

@@ -16,18 +16,20 @@ def kept_positions(idx, K, grid, start):
     return torch.tensor(cols, dtype=torch.int64).reshape(-1, 3).t()
 
 
-TWO_PI = Fraction("6.28318530717958647692528676655900576839433879875021")
-BITS = 200
+SCALE = 1 << 150
+TURN = round(Fraction("6.28318530717958647692528676655900576839433879875021") * SCALE)
 
 
 def angles(pos, inv_freq, pair_axis):
-    """[tokens, pairs] angles; pos int [axes, tokens].  Whole turns are taken out
-    in integers of 2^-200 of a turn first, so that large positions keep their bits."""
+    """[tokens, pairs] angles, the fp32 products of positions and frequencies; pos
+    int [axes, tokens].  Whole turns are taken out in integers of 2^-150, so that
+    large angles keep their bits."""
     out = torch.empty(pos.shape[1], len(inv_freq), dtype=torch.float64)
     for i, (f, a) in enumerate(zip(inv_freq, pair_axis)):
-        turn = round(Fraction(f) / TWO_PI * (1 << BITS))
-        out[:, i] = torch.tensor([(p * turn % (1 << BITS)) / (1 << BITS) for p in pos[a].tolist()], dtype=torch.float64)
-    return out * (2.0 * math.pi)
+        z = pos[a].float() * torch.tensor(f, dtype=torch.float32)
+        ratios = [v.as_integer_ratio() for v in z.double().tolist()]
+        out[:, i] = torch.tensor([(n * (SCALE // d) % TURN) / SCALE for n, d in ratios], dtype=torch.float64)
+    return out
 
 
 def pairs(rot_dim, adjacent):
