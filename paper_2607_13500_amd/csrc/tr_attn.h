@@ -63,9 +63,19 @@ hipError_t launch_rotate(const RotateArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_rotate_backward(const RotateArgs& a, bool bf16, hipStream_t s);
 
 // ---- attention ---------------------------------------------------------------
+// Division of x < 2^31 by a number fixed for a launch: (mulhi(x, mul) + x) >> shift.
+struct Divisor {
+    uint32_t mul, shift;
+};
+
 struct AttendArgs {
     int64_t tokens;
     int32_t heads, kv_heads, dim;
+    int32_t group;             // heads / kv_heads
+    Divisor by_group, by_page;
+    int32_t most;              // tokens that a row of the table has pages for
+    int32_t least;             // steps of a workgroup's share, at least
+    float* part;               // attend_part_floats of scratch
     tr_heads q, out;
     tr_cache cache;
     tr_step step;
@@ -75,6 +85,8 @@ struct AttendArgs {
     int32_t cus;
 };
 
+// group, the divisors, most, least and scale's power are filled in by the launch.
+size_t attend_part_floats(int dim, int cus);
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
 
 // ---- device helpers ------------------------------------------------------------

@@ -29,6 +29,7 @@ struct tr_attn {
     float* freq = nullptr;          // [rot_dim / 2], see RotateArgs
     int32_t* pair_axis = nullptr;   // [rot_dim / 2]
     float* part = nullptr;          // partial sums of dw
+    float* parts = nullptr;         // parts of rows that several workgroups attend for (bf16)
 };
 
 namespace {
@@ -204,6 +205,11 @@ tr_status tr_attn_create(const tr_attn_params* p, tr_attn** out)
     if ((e = al(&a->freq, sizeof freq)) != hipSuccess || (e = al(&a->pair_axis, sizeof axis)) != hipSuccess ||
         (e = al(&a->part, tr::rotate_part_floats(p->head_dim, a->cus) * sizeof(float))) != hipSuccess) {
         tr_attn_destroy(a);
+        return fail(TR_ENOMEM, "hipMalloc of a layer's tables failed: %s", hipGetErrorString(e));
+    }
+    if (p->dtype == TR_BF16 && p->head_dim % 8 == 0 &&
+        (e = al(&a->parts, tr::attend_part_floats(p->head_dim, a->cus) * sizeof(float))) != hipSuccess) {
+        tr_attn_destroy(a);
         return fail(TR_ENOMEM, "hipMalloc of a layer's scratch failed: %s", hipGetErrorString(e));
     }
     if ((e = hipMemcpy(a->freq, freq, sizeof freq, hipMemcpyHostToDevice)) != hipSuccess ||
@@ -226,6 +232,7 @@ void tr_attn_destroy(tr_attn* a)
     if (a->freq) (void)hipFree(a->freq);
     if (a->pair_axis) (void)hipFree(a->pair_axis);
     if (a->part) (void)hipFree(a->part);
+    if (a->parts) (void)hipFree(a->parts);
     delete a;
 }
 
@@ -422,6 +429,7 @@ tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const 
     r.causal = causal;
     r.window = window;
     r.lse = lse;
+    r.part = a->parts;
     r.cus = a->cus;
     hipError_t e = tr::launch_attend(r, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
