@@ -96,8 +96,10 @@ __device__ __forceinline__ void seen_by(const AttendArgs& a, const Sequence& s, 
 // values in flight, in registers, while it works on one; 16 rows cost two
 // matrix instructions of 16 cycles per 16 x 32 elements of keys.
 constexpr int kRows = 16, kTile = 32, kStep = 128, kFewThreads = 256;
+constexpr int kAlign = 32;   // a range of keys begins at a multiple of it
 
-// Where a workgroup is in the row of all steps.
+// Where a workgroup is in the row of all steps.  Items of a sequence are its
+// tiles of ROWS rows, and of each the key heads one after another.
 struct Place {
     int b;             // sequence
     Sequence s;
@@ -106,40 +108,46 @@ struct Place {
     int64_t first;     // its first step in the row
 };
 
+// Steps of STEP keys that an item of a sequence takes (STEP 0: an item is one step).
+template <int STEP>
 __device__ __forceinline__ int steps_of(const Sequence& s)
 {
-    return max(1, (s.end - (s.begin & ~(kTile - 1)) + kStep - 1) / kStep);
+    if constexpr (STEP == 0) return 1;
+    else return max(1, (s.end - (s.begin & ~(kAlign - 1)) + STEP - 1) / STEP);
 }
 
+template <int ROWS>
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, const Sequence& s)
+{
+    return (int)(((int64_t)s.n * a.group + ROWS - 1) / ROWS);
+}
+
+template <int ROWS, int STEP>
 __device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b)
 {
     if (b >= a.step.seqs) return 0;
     const Sequence s = sequence_at(a, b);
-    const int64_t tiles = ((int64_t)s.n * a.group + kRows - 1) / kRows;
-    return tiles * steps_of(s) * a.kv_heads;
+    return (int64_t)tiles_of<ROWS>(a, s) * steps_of<STEP>(s) * a.kv_heads;
 }
 
-__device__ __forceinline__ int64_t wave_sum_i64(int64_t x)
-{
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    return x;
-}
-
+template <int ROWS, int STEP>
 __device__ __forceinline__ int64_t all_steps(const AttendArgs& a, int lane)
 {
     int64_t sum = 0;
-    for (int b0 = 0; b0 < a.step.seqs; b0 += 64) sum += cost_of(a, b0 + lane);
-    return uniform(wave_sum_i64(sum));
+    for (int b0 = 0; b0 < a.step.seqs; b0 += 64) sum += cost_of<ROWS, STEP>(a, b0 + lane);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+    return uniform(sum);
 }
 
 // The sequence that step u (< all_steps) lies in.
+template <int ROWS, int STEP>
 __device__ __forceinline__ Place place_of(const AttendArgs& a, int64_t u, int lane)
 {
     Place p{};
     int64_t before = 0;
     for (int b0 = 0; b0 < a.step.seqs; b0 += 64) {
-        const int64_t c = cost_of(a, b0 + lane);
+        const int64_t c = cost_of<ROWS, STEP>(a, b0 + lane);
         int64_t sum = c;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -157,8 +165,8 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int64_t u, int la
     }
     p.b = __builtin_amdgcn_readfirstlane(p.b);
     p.s = sequence_at(a, p.b);
-    p.steps = steps_of(p.s);
-    p.tiles = (int)(((int64_t)p.s.n * a.group + kRows - 1) / kRows);
+    p.steps = steps_of<STEP>(p.s);
+    p.tiles = tiles_of<ROWS>(a, p.s);
     return p;
 }
 
@@ -185,9 +193,9 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, int64_t t, int h
     if (a.lse && e0 == 0) a.lse[t * a.heads + head] = some ? fmaf(m, kLn2, __logf(l)) : minus_inf();
 }
 
-// Floats of one part in the scratch: 16 rows of DH sums, their maxima and l.
-template <int DH>
-constexpr int kPartFloats = kRows * DH + 2 * kRows;
+// Floats of one part in the scratch: ROWS rows of DH sums, their maxima and l.
+template <int DH, int ROWS>
+constexpr int kPartFloats = ROWS * DH + 2 * ROWS;
 
 // Address swizzle of a row of V in shared memory, in pieces of 16 bytes: the 16
 // rows that a transposing read touches spread over all banks.
@@ -221,18 +229,18 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
     const int token_bytes = (int)(a.cache.token * 2);            // PG16
     const int k_lane = col * token_bytes + grp * 16, v_lane = vrow * token_bytes + piece * 16;
 
-    const int64_t total = all_steps(a, lane);
+    const int64_t total = all_steps<kRows, kStep>(a, lane);
     const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
     int64_t u = (int64_t)blockIdx.x * share;
     const int64_t u_end = min(u + share, total);
 
     while (u < u_end) {
-        const Place pl = place_of(a, u, lane);
+        const Place pl = place_of<kRows, kStep>(a, u, lane);
         const Sequence s = pl.s;
         const int64_t local = u - pl.first;
         const int item = (int)(local / pl.steps), step0 = (int)(local - (int64_t)item * pl.steps);
         const int step1 = (int)min((int64_t)pl.steps, step0 + (u_end - u));
-        const int h = item / pl.tiles, rt = item - h * pl.tiles;
+        const int rt = item / a.kv_heads, h = item - rt * a.kv_heads;
         const bool whole = step0 == 0 && step1 == pl.steps;
 
         // ---- this lane's row ------------------------------------------------------
@@ -460,7 +468,7 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
                     const int t = (int)divide(rr, a.by_group), hd = h * a.group + (int)(rr - (uint32_t)t * a.group);
                     finish_row<N>(a, s.q0 + t, hd, e0, acc, sum, top);
                 } else {
-                    float* part = a.part + ((int64_t)blockIdx.x * 2 + (step0 == 0)) * kPartFloats<DH>;
+                    float* part = a.part + ((int64_t)blockIdx.x * 2 + (step0 == 0)) * kPartFloats<DH, kRows>;
 #pragma unroll
                     for (int e = 0; e < N; ++e) part[row * DH + e0 + e] = acc[e];
                     if (e0 == 0) {
@@ -476,45 +484,45 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
 }
 
 // Joins the parts of each item that several workgroups worked on: workgroup i
-// does the item that began in attend_few_kernel's workgroup i and went on past
-// it, whose later parts are the first ones of the workgroups after i.  One
-// wavefront a row.
-template <int DH>
+// does the item that began in workgroup i of the kernel before (of `groups`)
+// and went on past it, whose later parts are the first ones of the workgroups
+// after i.  One wavefront a row, 16 rows of the item to a workgroup.
+template <int DH, int ROWS, int STEP>
 __global__ __launch_bounds__(1024) void join_kernel(AttendArgs a)
 {
     constexpr int N = DH / 64;
-    const int lane = threadIdx.x & 63, row = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t total = all_steps(a, lane);
+    const int lane = threadIdx.x & 63, row = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + 16 * blockIdx.y;
+    const int64_t total = all_steps<ROWS, STEP>(a, lane);
     const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
     const int64_t u0 = (int64_t)blockIdx.x * share, u1 = u0 + share;
     if (u1 >= total) return;                          // nothing goes on past the last share
-    const Place pl = place_of(a, u1 - 1, lane);
+    const Place pl = place_of<ROWS, STEP>(a, u1 - 1, lane);
     const int64_t local = u1 - 1 - pl.first;
     const int item = (int)(local / pl.steps);
     const int64_t begin = pl.first + (int64_t)item * pl.steps, end = begin + pl.steps;
     if (begin < u0 || end <= u1) return;              // not begun here, or done here
-    const int h = item / pl.tiles, rt = item - h * pl.tiles;
-    const int rows = (int)min((int64_t)kRows, (int64_t)pl.s.n * a.group - (int64_t)rt * kRows);
+    const int rt = item / a.kv_heads, h = item - rt * a.kv_heads;
+    const int rows = (int)min((int64_t)ROWS, (int64_t)pl.s.n * a.group - (int64_t)rt * ROWS);
     if (row >= rows) return;
     const int parts = (int)((end - 1) / share - (int64_t)blockIdx.x) + 1;
     // part 0 is this workgroup's second, the others are the first of theirs
-    auto part = [&](int i) { return a.part + (((int64_t)blockIdx.x + i) * 2 + (i == 0)) * kPartFloats<DH>; };
+    auto part = [&](int i) { return a.part + (((int64_t)blockIdx.x + i) * 2 + (i == 0)) * kPartFloats<DH, ROWS>; };
     float top = minus_inf();
-    for (int i = lane; i < parts; i += 64) top = fmaxf(top, part(i)[kRows * DH + row]);
+    for (int i = lane; i < parts; i += 64) top = fmaxf(top, part(i)[ROWS * DH + row]);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
     const float zero = top == minus_inf() ? 0.f : top;
     float sum = 0.f, acc[N] = {};
     for (int i = 0; i < parts; ++i) {
         const float* p = part(i);
-        const float f = exp2_(p[kRows * DH + row] - zero);
-        sum = fmaf(p[kRows * DH + kRows + row], f, sum);
+        const float f = exp2_(p[ROWS * DH + row] - zero);
+        sum = fmaf(p[ROWS * DH + ROWS + row], f, sum);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] = fmaf(p[row * DH + lane * N + e], f, acc[e]);
     }
-    const uint32_t r = (uint32_t)(rt * kRows + row);
+    const uint32_t r = (uint32_t)rt * ROWS + row;
     const int t = (int)divide(r, a.by_group), head = h * a.group + (int)(r - (uint32_t)t * a.group);
-    // a lane's N elements as two or more: neighbours' are fetched where N is 1
+    // a lane's N elements as two or more: a neighbour's is fetched where N is 1
     if constexpr (N == 1) {
         const float next = __shfl_down(acc[0], 1);
         const float two[2] = {acc[0], next};
@@ -524,6 +532,309 @@ __global__ __launch_bounds__(1024) void join_kernel(AttendArgs a)
     }
 }
 
+// ---- many rows ---------------------------------------------------------------------------
+// A workgroup of NW wavefronts of 32 rows each over the same keys, in tiles of
+// 64 that go from memory straight into shared memory, two tiles there at a time:
+// one is loaded while the other is worked on.
+//
+// Shared memory rows are DH elements in pieces of 16 bytes; piece c of row r lies
+// at piece c ^ f(r), which the loads bring about by each lane's choice of source
+// (they fill shared memory in lane order).  f spreads the rows that one read of
+// 16 (keys) or 4 (values) rows touches over all banks.
+constexpr int kManyTile = 64, kManyRows = 32;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int DH>
+__device__ __forceinline__ int k_swizzle(int row)
+{
+    return DH == 64 ? (row >> 1) & 7 : row & 15;
+}
+
+template <int DH>
+__device__ __forceinline__ int v_swizzle(int row)
+{
+    return DH == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
+}
+
+// 16 bytes a lane from memory into shared memory at lds + 16 lane.  An
+// instruction without a register result: the kernel counts and waits itself.
+__device__ __forceinline__ void load_lds(uint32_t lds, const void* p)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
+}
+
+__device__ __forceinline__ void wait_all_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ float max_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int DH, int NW, int STEP, bool FULL>
+__global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel(AttendArgs a)
+{
+    constexpr int ROWS = NW * kManyRows, T = NW * 64;
+    constexpr int KF = DH / 16, DT = DH / 32;               // fragments of keys, tiles of elements
+    constexpr int PIECES = DH / 8, BYTES = kManyTile * DH * 2;
+    constexpr int LR = T / PIECES, NI = kManyTile / LR;     // rows of one round of loads, rounds of a tile
+    __shared__ __align__(16) unsigned char smem[4 * BYTES]; // stage 0: K, V; stage 1: K, V
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    const int lrow = threadIdx.x / PIECES, lpos = threadIdx.x % PIECES;
+
+    const int64_t total = all_steps<ROWS, STEP>(a, lane);
+    int64_t u, u_end;
+    if constexpr (STEP == 0) {
+        // one item a workgroup, the last ones (which see most) first
+        u = total - 1 - (int64_t)blockIdx.x;
+        if (u < 0) return;
+        u_end = u + 1;
+    } else {
+        const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
+        u = (int64_t)blockIdx.x * share;
+        u_end = min(u + share, total);
+    }
+    if constexpr (!FULL) {
+        for (int i = threadIdx.x; i < 4 * BYTES / 16; i += T) reinterpret_cast<u32x4*>(smem)[i] = u32x4{};   // pieces past the head stay zero
+        __syncthreads();
+    }
+    while (u < u_end) {
+        const Place pl = place_of<ROWS, STEP>(a, u, lane);
+        const Sequence s = pl.s;
+        const int64_t local = u - pl.first;
+        const int item = (int)(local / pl.steps), step0 = (int)(local - (int64_t)item * pl.steps);
+        const int step1 = (int)min((int64_t)pl.steps, step0 + (u_end - u));
+        const int rt = item / a.kv_heads, h = item - rt * a.kv_heads;
+        const bool whole = step0 == 0 && step1 == pl.steps;
+
+        // ---- rows: this lane's, the wavefront's and the workgroup's -------------------
+        const int rows = (int)min((int64_t)ROWS, (int64_t)s.n * a.group - (int64_t)rt * ROWS);
+        const int wrow = wave * kManyRows, my = wrow + col;
+        const bool live = my < rows;
+        const uint32_t r = (uint32_t)rt * ROWS + my;
+        const int tok = (int)divide(r, a.by_group), head = h * a.group + (int)(r - (uint32_t)tok * a.group);
+        int lo = 0, hi = 0;
+        if (live) seen_by(a, s, tok, lo, hi);
+        auto bounds = [&](int r0, int r1, int& lo0, int& hi0, int& lo1, int& hi1) {    // of rows r0 .. r1 of the tile
+            seen_by(a, s, (int)divide((uint32_t)rt * ROWS + r0, a.by_group), lo0, hi0);
+            seen_by(a, s, (int)divide((uint32_t)rt * ROWS + r1, a.by_group), lo1, hi1);
+        };
+        int lo_min, hi_min, lo_max, hi_max, wlo_min = 0, whi_min = 0, wlo_max = 0, whi_max = 0;
+        bounds(0, rows - 1, lo_min, hi_min, lo_max, hi_max);
+        const bool works = wrow < rows;
+        if (works) bounds(wrow, min(rows, wrow + kManyRows) - 1, wlo_min, whi_min, wlo_max, whi_max);
+        const bool full_rows = wrow + kManyRows <= rows;
+
+        bf16x8 qf[KF];
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+            u32x4 v{};
+            if (live && (FULL || k * 16 + half * 8 < a.dim))
+                v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q.p) + (s.q0 + tok) * a.q.token + (int64_t)head * a.q.head + k * 16 + half * 8);
+            v = (v & a.keep) ^ a.flip;            // scale < 0: that of -q; scale 0: scores of q = 0
+            qf[k] = __builtin_bit_cast(bf16x8, v);
+        }
+        f32x16 o[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
+        float m = minus_inf(), l = 0.f;           // m: of the scores before their scale
+
+        // ---- keys ---------------------------------------------------------------------
+        const int base = s.begin & ~(kAlign - 1);
+        int j0 = base + step0 * STEP;
+        if (lo_min > j0) j0 += (lo_min - j0) / kManyTile * kManyTile;   // tiles that no row sees are skipped
+        const int j_end = STEP == 0 ? hi_max : min(hi_max, base + step1 * STEP);
+        const int last = hi_max - 1;
+        const int32_t* table = a.step.table + (int64_t)pl.b * a.step.table_stride;
+        const uint16_t* kp = static_cast<const uint16_t*>(a.cache.k) + (int64_t)h * a.cache.head;
+        const uint16_t* vp = static_cast<const uint16_t*>(a.cache.v) + (int64_t)h * a.cache.head;
+        int page[NI], in[NI];
+        auto pages = [&](int j) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                // rows that no row of the tile sees are read as the nearest that one does
+                const int t = min(max(j + i * LR + lrow, lo_min), last);
+                const int slot = (int)divide((uint32_t)t, a.by_page);
+                page[i] = table[slot];
+                in[i] = t - slot * a.cache.page_size;
+            }
+        };
+        auto load = [&](int stage) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int row = i * LR + lrow;
+                const int64_t at = (int64_t)min(max(page[i], 0), a.cache.pages - 1) * a.cache.page + (int64_t)in[i] * a.cache.token;
+                const int kc = (lpos ^ k_swizzle<DH>(row)) * 8, vc = (lpos ^ v_swizzle<DH>(row)) * 8;
+                const uint32_t to = lds0 + stage * 2 * BYTES + (i * T + wave * 64) * 16;
+                if (FULL || kc < a.dim) load_lds(to, kp + at + kc);
+                if (FULL || vc < a.dim) load_lds(to + BYTES, vp + at + vc);
+            }
+        };
+        if (j0 < j_end) {
+            pages(j0);
+            load(0);
+            if (j0 + kManyTile < j_end) pages(j0 + kManyTile);
+        }
+        int stage = 0;
+        for (; j0 < j_end; j0 += kManyTile, stage ^= 1) {
+            wait_all_loads();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            if (j0 + kManyTile < j_end) {
+                load(stage ^ 1);
+                if (j0 + 2 * kManyTile < j_end) pages(j0 + 2 * kManyTile);
+            }
+            const unsigned char* kt = smem + stage * 2 * BYTES;
+            unsigned char* vt = smem + stage * 2 * BYTES + BYTES;
+
+            // a value that is not finite must not reach rows that do not see it
+            bool bad = false;
+            if (lo_max > max(j0, lo_min) || hi_min < min(j0 + kManyTile, hi_max)) {
+                bool mine = false;
+                for (int i = threadIdx.x; i < BYTES / 16; i += T) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(vt + i * 16);
+                    mine |= not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
+                }
+                bad = __syncthreads_or(mine);
+            }
+            const bool idle = !works || j0 >= whi_max || j0 + kManyTile <= wlo_min;
+            if (idle && !bad) continue;
+
+            f32x16 sc[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[x][v] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KF; ++k) {
+                    const int row = 32 * x + col;
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + row * (DH * 2) + ((2 * k + half) ^ k_swizzle<DH>(row)) * 16);
+                    sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], sc[x], 0, 0, 0);
+                }
+            }
+            if (!full_rows || j0 < wlo_max || j0 + kManyTile > whi_min) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int j = j0 + 32 * x + 8 * (v / 4) + 4 * half + v % 4;
+                        sc[x][v] = j >= lo && j < hi ? sc[x][v] : minus_inf();
+                    }
+            }
+            float top = minus_inf();
+#pragma unroll
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, fmaxf(sc[0][v], sc[1][v]));
+            top = max_halves(top);
+            // The maximum that a row's weights are relative to follows only when it is
+            // left behind by 2^8: sums scaled by less than that lose nothing.
+            const bool left = (top - m) * a.scale > 8.f;
+            if (__any(left)) {
+                const float keep = left ? exp2_((m - top) * a.scale) : 1.f;
+                m = left ? top : m;
+                l *= keep;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] *= keep;
+            }
+            const float zero = m == minus_inf() ? 0.f : m * a.scale;
+            s16x8 pb[4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float p = exp2_(fmaf(sc[x][v], a.scale, -zero));
+                    l += p;
+                    pb[2 * x + v / 8][v % 8] = (short)to_bf16(p);
+                }
+            if (bad) {
+                // such values go to the rows that see them, key by key, and count as
+                // zeros in the product
+#pragma unroll 1
+                for (int i = 0; i < kManyTile; ++i) {
+                    // key i lies in half (i / 4) % 2, element 4 ((i / 8) % 2) + i % 4 of pb[i / 16]
+                    uint32_t w = 0;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int v = 0; v < 8; ++v)
+                            w = x == i >> 4 && v == (i >> 3 & 1) * 4 + (i & 3) ? (uint32_t)(uint16_t)pb[x][v] : w;
+                    const float p = from_bf16(__shfl(w, (i & 4) * 8 + col));
+                    const bool sees = j0 + i >= lo && j0 + i < hi;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const int e = 32 * d + 8 * v + 4 * half;
+                            const uint16_t* q = reinterpret_cast<const uint16_t*>(vt + i * (DH * 2) + ((e / 8) ^ v_swizzle<DH>(i)) * 16) + e % 8;
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                const float z = fmaf(p, from_bf16(q[y]), o[d][4 * v + y]);
+                                o[d][4 * v + y] = sees && not_finite(q[y]) ? z : o[d][4 * v + y];
+                            }
+                        }
+                }
+                __syncthreads();
+                for (int i = threadIdx.x; i < BYTES / 2; i += T) {
+                    uint16_t* q = reinterpret_cast<uint16_t*>(vt) + i;
+                    if (not_finite(*q)) *q = 0;
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    s16x8 vf;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int row = 16 * c + 8 * y + 4 * half + (lane & 15) / 4;
+                        const int e = 32 * d + (lane & 16) + 4 * (lane & 3);
+                        const unsigned char* q = vt + row * (DH * 2) + ((e / 8) ^ v_swizzle<DH>(row)) * 16 + (e % 8) * 2;
+                        const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) vf[4 * y + v] = t[v];
+                    }
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pb[c]), o[d], 0, 0, 0);
+                }
+        }
+
+        // ---- results: a lane holds 4 elements after another of its row -------------------
+        l += __shfl_xor(l, 32);
+        if (live) {
+            const float top = m == minus_inf() ? m : m * a.scale;
+            if (whole) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float acc[4] = {o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]};
+                        finish_row<4>(a, s.q0 + tok, head, 32 * d + 8 * v + 4 * half, acc, l, top);
+                    }
+            } else {
+                float* part = a.part + ((int64_t)blockIdx.x * 2 + (step0 == 0)) * kPartFloats<DH, ROWS>;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        *reinterpret_cast<f32x4*>(part + my * DH + 32 * d + 8 * v + 4 * half) =
+                            f32x4{o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]};
+                if (half == 0) {
+                    part[ROWS * DH + my] = top;
+                    part[ROWS * DH + ROWS + my] = l;
+                }
+            }
+        }
+        __syncthreads();      // the tiles in shared memory are free
+        u += step1 - step0;
+    }
+}
+
+// ---- launches ------------------------------------------------------------------------------
 Divisor divisor(uint32_t d)
 {
     Divisor v;
@@ -545,17 +856,57 @@ hipError_t few(const AttendArgs& a, hipStream_t s)
     hipError_t e = a.dim == DH ? (pg16 ? launch(attend_few_kernel<DH, true, true>) : launch(attend_few_kernel<DH, false, true>))
                                : (pg16 ? launch(attend_few_kernel<DH, true, false>) : launch(attend_few_kernel<DH, false, false>));
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(join_kernel<DH>, grid, dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((join_kernel<DH, kRows, kStep>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
+}
+
+// Wavefronts of a workgroup of the kernel for many rows, and its workgroups of a
+// CU when items are shared.
+template <int DH>
+constexpr int kManyWaves = DH == 256 ? 4 : 8;
+constexpr int kManyStep = 256;
+
+template <int DH>
+hipError_t many(const AttendArgs& a, hipStream_t s)
+{
+    constexpr int NW = kManyWaves<DH>, ROWS = NW * kManyRows;
+    // no more items than this, whatever the sequences' lengths
+    const int64_t items = ((a.tokens * a.group + ROWS - 1) / ROWS + a.step.seqs) * a.kv_heads;
+    auto launch = [&](auto kernel, int64_t groups) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(NW * 64), 0, s, a);
+        return hipGetLastError();
+    };
+    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus)
+        return a.dim == DH ? launch(attend_many_kernel<DH, NW, 0, true>, items) : launch(attend_many_kernel<DH, NW, 0, false>, items);
+    hipError_t e = a.dim == DH ? launch(attend_many_kernel<DH, NW, kManyStep, true>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false>, a.cus);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((join_kernel<DH, ROWS, kManyStep>), dim3((unsigned)a.cus, ROWS / 16), dim3(1024), 0, s, a);
+    return hipGetLastError();
+}
+
+template <int DH>
+constexpr size_t kGroupFloats = 2 * std::max(kFewPerCu<DH> * kPartFloats<DH, kRows>, kPartFloats<DH, kManyWaves<DH> * kManyRows>);
+
+template <int DH>
+hipError_t attend(const AttendArgs& args, hipStream_t s)
+{
+    AttendArgs a = args;
+    if (a.tokens * a.group <= 32 * (int64_t)a.step.seqs) {
+        a.scale = a.raw_scale * kLog2e;
+        return few<DH>(a, s);
+    }
+    a.scale = fabsf(a.raw_scale) * kLog2e;
+    a.flip = a.raw_scale < 0.f ? 0x80008000u : 0u;
+    a.keep = a.scale > 0.f ? ~0u : 0u;
+    if (!a.keep) a.scale = 1.f;
+    return many<DH>(a, s);
 }
 
 }  // namespace
 
 size_t attend_part_floats(int dim, int cus)
 {
-    const size_t groups = (size_t)2 * cus;            // two parts for each workgroup of a CU
-    return groups * (dim <= 64 ? kFewPerCu<64> * kPartFloats<64> : dim <= 128 ? kFewPerCu<128> * kPartFloats<128>
-                                                                           : kFewPerCu<256> * kPartFloats<256>);
+    return (size_t)cus * (dim <= 64 ? kGroupFloats<64> : dim <= 128 ? kGroupFloats<128> : kGroupFloats<256>);
 }
 
 hipError_t launch_attend(const AttendArgs& args, hipStream_t s)
@@ -565,9 +916,8 @@ hipError_t launch_attend(const AttendArgs& args, hipStream_t s)
     a.by_group = divisor((uint32_t)a.group);
     a.by_page = divisor((uint32_t)a.cache.page_size);
     a.most = (int32_t)std::min((int64_t)a.step.table_width * a.cache.page_size, (int64_t)INT32_MAX - 4096);
-    a.scale *= kLog2e;
     a.least = 1;
-    return a.dim <= 64 ? few<64>(a, s) : a.dim <= 128 ? few<128>(a, s) : few<256>(a, s);
+    return a.dim <= 64 ? attend<64>(a, s) : a.dim <= 128 ? attend<128>(a, s) : attend<256>(a, s);
 }
 
 }  // namespace tr

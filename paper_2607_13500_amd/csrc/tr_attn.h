@@ -79,13 +79,15 @@ struct AttendArgs {
     tr_heads q, out;
     tr_cache cache;
     tr_step step;
-    float scale;               // of the scores
+    float raw_scale;           // of the scores
+    float scale;               // the same in powers of two
+    uint32_t keep, flip;       // bits of q to keep and then to flip, where scale has to be > 0
     int32_t causal, window;
     float* lse;                // [tokens, heads] or nullptr
     int32_t cus;
 };
 
-// group, the divisors, most, least and scale's power are filled in by the launch.
+// group, the divisors, most, least, scale, keep and flip are filled in by the launch.
 size_t attend_part_floats(int dim, int cus);
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
 

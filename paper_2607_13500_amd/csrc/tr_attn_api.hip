@@ -406,6 +406,8 @@ tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const 
     if (window < 0 || (window > 0 && !causal))
         return fail(TR_EINVAL, "window must be >= 0, and 0 without causal (got %d)", window);
     if (T == 0) return TR_OK;
+    if (T * (a->p.heads / a->p.kv_heads) > kMaxTokens - 65536)
+        return fail(TR_EUNSUPPORTED, "T times the queries of a key head must stay below 2^31 - 65536");
     const int dim = a->p.head_dim;
     if ((st = check_cache(a, c, s)) != TR_OK || (st = check_heads("q", q, a->eb, T, a->p.heads)) != TR_OK ||
         (st = check_out_heads("out", out, a->eb, T, a->p.heads, dim)) != TR_OK)
@@ -425,7 +427,7 @@ tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const 
     r.out = out;
     r.cache = *c;
     r.step = *s;
-    r.scale = (float)scale;
+    r.raw_scale = (float)scale;
     r.causal = causal;
     r.window = window;
     r.lse = lse;
