@@ -20,8 +20,6 @@
 namespace tr {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 // ---- positions -----------------------------------------------------------------
 __global__ __launch_bounds__(256) void positions_kernel(PosArgs a)
 {
@@ -302,66 +300,72 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(RotateArgs g, int parts
     }
 }
 
-// ---- heads of whole 16-byte pieces: LP lanes a head --------------------------------
-// Lane j of the LP that share a head holds two 16-byte pieces of it: the first
-// and the second elements of C pairs (or, where pairs are adjacent, C pairs one
-// after another), and past the rotated part any two pieces.  All the lanes of a
-// group keep their sines and cosines while the wavefront walks over a token's
-// heads, 64 / LP at a time.
+// ---- heads of whole pieces: LP lanes a head ----------------------------------------
+// Lane j of the LP that share a head holds two pieces of four elements: the first
+// and the second elements of four pairs (or, where pairs are adjacent, four pairs
+// one after another), and past the rotated part any two pieces.  All the lanes of
+// a group keep their sines and cosines while the wavefront walks over a token's
+// heads, 64 / LP at a time, with DEPTH rounds of loads in flight.  Pieces of eight
+// bf16 elements need twice the registers (fewer wavefronts) and, as each group
+// works all angles out, twice the sines: 36864 tokens of 40 bf16 heads of 128
+// took 190 us.
+constexpr int kPiece = 4;
+
 template <typename E>
+using Raw = uint32_t __attribute__((ext_vector_type(sizeof(E))));   // a piece as it lies in memory
+
 struct Piece {
-    static constexpr int C = 16 / (int)sizeof(E);
-    float a[C], b[C];   // of pair i: a[i], b[i]; past the rotated part: the two pieces
+    float a[kPiece], b[kPiece];   // of pair i: a[i], b[i]; past the rotated part: the two pieces
 };
 
 template <typename E, bool ADJ>
-__device__ __forceinline__ Piece<E> unpack(u32x4 x, u32x4 y)
+__device__ __forceinline__ Piece unpack(Raw<E> x, Raw<E> y)
 {
-    constexpr int C = Piece<E>::C;
-    Piece<E> p;
-    float v[2 * C];
+    Piece p;
+    float v[2 * kPiece];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w0 = x[i], w1 = y[i];
-        if constexpr (C == 8) {
-            v[2 * i] = __uint_as_float(w0 << 16);
-            v[2 * i + 1] = __uint_as_float(w0 & 0xffff0000u);
-            v[C + 2 * i] = __uint_as_float(w1 << 16);
-            v[C + 2 * i + 1] = __uint_as_float(w1 & 0xffff0000u);
+    for (int i = 0; i < kPiece; ++i) {
+        if constexpr (sizeof(E) == 2) {
+            v[i] = __uint_as_float(i & 1 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16);
+            v[kPiece + i] = __uint_as_float(i & 1 ? y[i / 2] & 0xffff0000u : y[i / 2] << 16);
         } else {
-            v[i] = __uint_as_float(w0);
-            v[C + i] = __uint_as_float(w1);
+            v[i] = __uint_as_float(x[i]);
+            v[kPiece + i] = __uint_as_float(y[i]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
+    for (int i = 0; i < kPiece; ++i) {
         p.a[i] = ADJ ? v[2 * i] : v[i];
-        p.b[i] = ADJ ? v[2 * i + 1] : v[C + i];
+        p.b[i] = ADJ ? v[2 * i + 1] : v[kPiece + i];
     }
     return p;
 }
 
 template <typename E, bool ADJ>
-__device__ __forceinline__ void pack(const Piece<E>& p, u32x4& x, u32x4& y)
+__device__ __forceinline__ void pack(const Piece& p, Raw<E>& x, Raw<E>& y)
 {
-    constexpr int C = Piece<E>::C;
-    float v[2 * C];
+    float v[2 * kPiece];
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
+    for (int i = 0; i < kPiece; ++i) {
         v[ADJ ? 2 * i : i] = p.a[i];
-        v[ADJ ? 2 * i + 1 : C + i] = p.b[i];
+        v[ADJ ? 2 * i + 1 : kPiece + i] = p.b[i];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (C == 8) {
+    for (int i = 0; i < (int)sizeof(E); ++i) {
+        if constexpr (sizeof(E) == 2) {
             x[i] = (uint32_t)narrow<E>(v[2 * i]) | (uint32_t)narrow<E>(v[2 * i + 1]) << 16;
-            y[i] = (uint32_t)narrow<E>(v[C + 2 * i]) | (uint32_t)narrow<E>(v[C + 2 * i + 1]) << 16;
+            y[i] = (uint32_t)narrow<E>(v[kPiece + 2 * i]) | (uint32_t)narrow<E>(v[kPiece + 2 * i + 1]) << 16;
         } else {
             x[i] = __float_as_uint(v[i]);
-            y[i] = __float_as_uint(v[C + i]);
+            y[i] = __float_as_uint(v[kPiece + i]);
         }
     }
 }
+
+template <typename E>
+__device__ __forceinline__ Raw<E> load(const E* p) { return *reinterpret_cast<const Raw<E>*>(p); }
+template <typename E>
+__device__ __forceinline__ void store(E* p, Raw<E> v) { *reinterpret_cast<Raw<E>*>(p) = v; }
 
 // Sum over each group of LP lanes, the same bits in all of them.
 template <int LP>
@@ -378,9 +382,10 @@ struct Spot {
     bool on, turns;
 };
 
-template <int C, bool ADJ>
+template <bool ADJ>
 __device__ __forceinline__ Spot spot_of(int j, int dim, int rot)
 {
+    constexpr int C = kPiece;
     Spot s;
     s.on = j < dim / (2 * C);
     s.turns = j < rot / (2 * C);
@@ -389,54 +394,48 @@ __device__ __forceinline__ Spot spot_of(int j, int dim, int rot)
     return s;
 }
 
-// What lane j's C pairs turn by: their frequencies, and two bits of axis each.
-template <int C>
+// What lane j's pairs turn by: their frequencies, and two bits of axis each.
 struct Spin {
-    float freq[C];
+    float freq[kPiece];
     uint32_t axes;
 };
 
-template <int C>
-__device__ __forceinline__ Spin<C> spin_of(const RotateArgs& g, int j, bool turns)
+__device__ __forceinline__ Spin spin_of(const RotateArgs& g, int j, bool turns)
 {
-    Spin<C> s;
+    Spin s;
     s.axes = 0;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        s.freq[i] = turns ? g.freq[C * j + i] : 0.f;
-        s.axes |= turns ? (uint32_t)g.pair_axis[C * j + i] << (2 * i) : 0u;
+    for (int i = 0; i < kPiece; ++i) {
+        s.freq[i] = turns ? g.freq[kPiece * j + i] : 0.f;
+        s.axes |= turns ? (uint32_t)g.pair_axis[kPiece * j + i] << (2 * i) : 0u;
     }
     return s;
 }
 
-// The C turns of a lane for token t (none: cosine 1, sine 0).
-template <int C>
-__device__ __forceinline__ void turns_of(const RotateArgs& g, const Spin<C>& spin, int64_t t, float (&c)[C], float (&s)[C])
+// A lane's turns for token t (none: cosine 1, sine 0).
+__device__ __forceinline__ void turns_of(const RotateArgs& g, const Spin& spin, int64_t t, Turn (&z)[kPiece])
 {
     static_assert(kMaxAxes == 4, "an axis is two bits");
     int32_t at[kMaxAxes];
 #pragma unroll
     for (int x = 0; x < kMaxAxes; ++x) at[x] = x < g.axes && g.rot ? g.pos[(int64_t)x * g.ldpos + t] : 0;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
+    for (int i = 0; i < kPiece; ++i) {
         const int32_t lo = spin.axes >> (2 * i) & 1u ? at[1] : at[0], hi = spin.axes >> (2 * i) & 1u ? at[3] : at[2];
-        const Turn z = turn_of(spin.axes >> (2 * i) & 2u ? hi : lo, spin.freq[i]);
-        c[i] = z.c;
-        s[i] = z.s;
-        __builtin_amdgcn_sched_barrier(0);   // one at a time: side by side they take twice the registers
+        z[i] = turn_of(spin.axes >> (2 * i) & 2u ? hi : lo, spin.freq[i]);
     }
 }
 
 template <typename E, bool ADJ>
-__device__ __forceinline__ Piece<E> load_weight(const void* w, const Spot& sp)
+__device__ __forceinline__ Piece load_weight(const void* w, const Spot& sp)
 {
-    Piece<E> p;
+    Piece p;
     if (w && sp.on) {
         const E* q = static_cast<const E*>(w);
-        return unpack<E, ADJ>(*reinterpret_cast<const u32x4*>(q + sp.e0), *reinterpret_cast<const u32x4*>(q + sp.e1));
+        return unpack<E, ADJ>(load(q + sp.e0), load(q + sp.e1));
     }
 #pragma unroll
-    for (int i = 0; i < Piece<E>::C; ++i) p.a[i] = p.b[i] = 1.f;
+    for (int i = 0; i < kPiece; ++i) p.a[i] = p.b[i] = 1.f;
     return p;
 }
 
@@ -444,93 +443,79 @@ __device__ __forceinline__ Piece<E> load_weight(const void* w, const Spot& sp)
 template <typename E, int LP, bool ADJ, bool APPEND>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int chunks)
 {
-    constexpr int C = Piece<E>::C, R = 64 / LP;
+    constexpr int R = 64 / LP, DEPTH = 4;
     const int lane = threadIdx.x & 63, j = lane & (LP - 1);
     const int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t = u / chunks;
     if (t >= g.tokens) return;
-    const int rows = g.heads[0] + g.heads[1] + g.heads[2];
-    const int first = (int)(u - t * chunks) * per * R + lane / LP;
-    const Spot sp = spot_of<C, ADJ>(j, g.dim, g.rot);
+    const int h0 = g.heads[0], h1 = h0 + g.heads[1], rows = h1 + g.heads[2];
+    const int begin = (int)(u - t * chunks) * per * R, end = min(rows, begin + per * R);   // the wavefront's heads
+    const Spot sp = spot_of<ADJ>(j, g.dim, g.rot);
 
-    // the head of row r: its side, and where it lies
-    auto source = [&](int r, int& kind) -> const E* {
-        int h = r;
-        kind = 0;
-        if (h >= g.heads[0]) {
-            h -= g.heads[0];
-            kind = 1;
-            if (APPEND && h >= g.heads[1]) {
-                h -= g.heads[1];
-                kind = 2;
-            }
-        }
-        const tr_heads& in = g.in[kind];
-        return static_cast<const E*>(in.p) + t * in.token + (int64_t)h * in.head;
-    };
-    u32x4 n0{}, n1{};
-    int kind_n = 0;
-    auto fetch = [&](int r) {
-        if (r < rows && sp.on) {
-            const E* p = source(r, kind_n);
-            n0 = *reinterpret_cast<const u32x4*>(p + sp.e0);
-            n1 = *reinterpret_cast<const u32x4*>(p + sp.e1);
+    Raw<E> x0[DEPTH], x1[DEPTH];
+    auto fetch = [&](int d, int r) {
+        if (r < end && sp.on) {
+            const int kind = r < h0 ? 0 : r < h1 ? 1 : 2;
+            const int h = kind == 0 ? r : kind == 1 ? r - h0 : r - h1;
+            const E* p = static_cast<const E*>(g.in[kind].p) + t * g.in[kind].token + (int64_t)h * g.in[kind].head;
+            x0[d] = load(p + sp.e0);
+            x1[d] = load(p + sp.e1);
         }
     };
-    fetch(first);
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) fetch(d, begin + d * R + lane / LP);
     int64_t row = 0;
     if constexpr (APPEND) {
         row = cache_row(g.step, g.cache, t, lane);
         if (row == kNoToken) return;
     }
-    float c[C], s[C];
-    turns_of<C>(g, spin_of<C>(g, j, sp.turns), t, c, s);
-    Piece<E> wq, wk;
+    Turn z[kPiece];
+    turns_of(g, spin_of(g, j, sp.turns), t, z);
+    Piece wq, wk;
     if (g.norm) {
         wq = load_weight<E, ADJ>(g.w[0], sp);
         wk = load_weight<E, ADJ>(g.w[1], sp);
     }
-    for (int i = 0; i < per; ++i) {
-        const int r = first + i * R;
-        if (__builtin_amdgcn_readfirstlane(r) >= rows) break;     // lane 0 holds the wavefront's first head
-        u32x4 x0 = n0, x1 = n1;
-        const int kind = kind_n;
-        if (i + 1 < per) fetch(r + R);
-        if (!APPEND || kind < 2) {
-            Piece<E> x = unpack<E, ADJ>(x0, x1);
-            if (g.norm) {
-                float q = 0.f;
+    for (int r0 = begin; r0 < end; r0 += DEPTH * R) {
 #pragma unroll
-                for (int e = 0; e < C; ++e) q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
-                q = group_sum<LP>(sp.on ? q : 0.f);
-                const float m = 1.f / sqrtf(q / (float)g.dim + g.eps);
+        for (int d = 0; d < DEPTH; ++d) {
+            if (r0 + d * R >= end) break;
+            const int r = r0 + d * R + lane / LP;
+            const int kind = r < h0 ? 0 : r < h1 ? 1 : 2;
+            Raw<E> y0 = x0[d], y1 = x1[d];
+            if (!APPEND || kind < 2) {
+                Piece x = unpack<E, ADJ>(y0, y1);
+                if (g.norm) {
+                    float q = 0.f;
 #pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    x.a[e] = x.a[e] * m * (kind ? wk.a[e] : wq.a[e]);
-                    x.b[e] = x.b[e] * m * (kind ? wk.b[e] : wq.b[e]);
+                    for (int e = 0; e < kPiece; ++e) q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
+                    q = group_sum<LP>(sp.on && r < end ? q : 0.f);
+                    const float m = 1.f / sqrtf(q / (float)g.dim + g.eps);
+#pragma unroll
+                    for (int e = 0; e < kPiece; ++e) {
+                        x.a[e] = x.a[e] * m * (kind ? wk.a[e] : wq.a[e]);
+                        x.b[e] = x.b[e] * m * (kind ? wk.b[e] : wq.b[e]);
+                    }
                 }
-            }
-            Piece<E> y = x;
-            if (sp.turns) {
+                Piece y = x;
+                if (sp.turns) {
 #pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    y.a[e] = fmaf(x.a[e], c[e], -(x.b[e] * s[e]));
-                    y.b[e] = fmaf(x.b[e], c[e], x.a[e] * s[e]);
+                    for (int e = 0; e < kPiece; ++e) {
+                        y.a[e] = fmaf(x.a[e], z[e].c, -(x.b[e] * z[e].s));
+                        y.b[e] = fmaf(x.b[e], z[e].c, x.a[e] * z[e].s);
+                    }
                 }
+                pack<E, ADJ>(y, y0, y1);
             }
-            pack<E, ADJ>(y, x0, x1);
-        }
-        if (r < rows && sp.on) {
-            const int h = r - (kind > 0 ? g.heads[0] : 0) - (kind > 1 ? g.heads[1] : 0);
-            E* p;
-            if (APPEND && kind > 0) {
-                if (row == kNoRow) continue;
-                p = static_cast<E*>(kind == 1 ? g.cache.k : g.cache.v) + row + (int64_t)h * g.cache.head;
-            } else {
-                p = static_cast<E*>(g.out[kind].p) + t * g.out[kind].token + (int64_t)h * g.out[kind].head;
+            fetch(d, r + DEPTH * R);
+            if (r < end && sp.on && !(APPEND && kind > 0 && row == kNoRow)) {
+                const int h = kind == 0 ? r : kind == 1 ? r - h0 : r - h1;
+                E* p;
+                if (APPEND && kind > 0) p = static_cast<E*>(kind == 1 ? g.cache.k : g.cache.v) + row + (int64_t)h * g.cache.head;
+                else p = static_cast<E*>(g.out[kind].p) + t * g.out[kind].token + (int64_t)h * g.out[kind].head;
+                store(p + sp.e0, y0);
+                store(p + sp.e1, y1);
             }
-            *reinterpret_cast<u32x4*>(p + sp.e0) = x0;
-            *reinterpret_cast<u32x4*>(p + sp.e1) = x1;
         }
     }
 }
@@ -539,83 +524,88 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int 
 // waves, ... and their heads, and keeps its lanes' share of dw, which a
 // workgroup joins into its row of `part`.
 template <typename E, int LP, bool ADJ>
-__global__ __launch_bounds__(256, 4) void rotate_back_kernel(RotateArgs g)
+__global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
 {
-    constexpr int C = Piece<E>::C, R = 64 / LP;
+    constexpr int R = 64 / LP, DEPTH = 2;
     __shared__ float red[4][kMaxHeadDim];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane & (LP - 1), kind = blockIdx.y;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & (LP - 1), kind = blockIdx.y;
     const int rows = g.heads[kind];
     const int64_t waves = (int64_t)gridDim.x * 4;
-    const Spot sp = spot_of<C, ADJ>(j, g.dim, g.rot);
+    const Spot sp = spot_of<ADJ>(j, g.dim, g.rot);
     const tr_heads hg = g.grad[kind], hx = g.in[kind], ho = g.out[kind];
-    const Spin<C> spin = spin_of<C>(g, j, sp.turns);
-    Piece<E> w, dw;
+    const Spin spin = spin_of(g, j, sp.turns);
+    Piece w, dw;
     if (g.norm) w = load_weight<E, ADJ>(g.w[kind], sp);
 #pragma unroll
-    for (int e = 0; e < C; ++e) dw.a[e] = dw.b[e] = 0.f;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(wave); t < g.tokens; t += waves) {
-        u32x4 g0{}, g1{}, x0{}, x1{};
-        auto fetch = [&](int r) {
+    for (int e = 0; e < kPiece; ++e) dw.a[e] = dw.b[e] = 0.f;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < g.tokens; t += waves) {
+        Raw<E> g0[DEPTH], g1[DEPTH], x0[DEPTH], x1[DEPTH];
+        auto fetch = [&](int d, int r) {
             if (r < rows && sp.on) {
                 const E* p = static_cast<const E*>(hg.p) + t * hg.token + (int64_t)r * hg.head;
-                g0 = *reinterpret_cast<const u32x4*>(p + sp.e0);
-                g1 = *reinterpret_cast<const u32x4*>(p + sp.e1);
+                g0[d] = load(p + sp.e0);
+                g1[d] = load(p + sp.e1);
                 if (g.norm) {
                     const E* q = static_cast<const E*>(hx.p) + t * hx.token + (int64_t)r * hx.head;
-                    x0 = *reinterpret_cast<const u32x4*>(q + sp.e0);
-                    x1 = *reinterpret_cast<const u32x4*>(q + sp.e1);
+                    x0[d] = load(q + sp.e0);
+                    x1[d] = load(q + sp.e1);
                 }
             }
         };
-        fetch(lane / LP);
-        float c[C], s[C];
-        turns_of<C>(g, spin, t, c, s);
-        for (int r = lane / LP; __builtin_amdgcn_readfirstlane(r) < rows; r += R) {
-            const bool live = r < rows && sp.on;
-            const Piece<E> d = unpack<E, ADJ>(g0, g1);
-            Piece<E> x;
-            if (g.norm) x = unpack<E, ADJ>(x0, x1);
-            fetch(r + R);
-            Piece<E> y = d;
-            if (sp.turns) {
 #pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    y.a[e] = fmaf(d.a[e], c[e], d.b[e] * s[e]);
-                    y.b[e] = fmaf(d.b[e], c[e], -(d.a[e] * s[e]));
-                }
-            }
-            if (g.norm) {
-                float q = 0.f, m = 0.f;
+        for (int d = 0; d < DEPTH; ++d) fetch(d, d * R + lane / LP);
+        Turn z[kPiece];
+        turns_of(g, spin, t, z);
+        for (int r0 = 0; r0 < rows; r0 += DEPTH * R) {
 #pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
-                    m = fmaf(y.a[e] * w.a[e], x.a[e], fmaf(y.b[e] * w.b[e], x.b[e], m));
-                }
-                q = group_sum<LP>(live ? q : 0.f);
-                m = group_sum<LP>(live ? m : 0.f);
-                const float n = 1.f / sqrtf(q / (float)g.dim + g.eps);
-                m = m * n / (float)g.dim;
+            for (int d = 0; d < DEPTH; ++d) {
+                if (r0 + d * R >= rows) break;
+                const int r = r0 + d * R + lane / LP;
+                const bool live = r < rows && sp.on;
+                Piece y = unpack<E, ADJ>(g0[d], g1[d]);
+                if (sp.turns) {
 #pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    const float ua = x.a[e] * n, ub = x.b[e] * n;
-                    dw.a[e] += live ? y.a[e] * ua : 0.f;
-                    dw.b[e] += live ? y.b[e] * ub : 0.f;
-                    y.a[e] = n * fmaf(-ua, m, y.a[e] * w.a[e]);
-                    y.b[e] = n * fmaf(-ub, m, y.b[e] * w.b[e]);
+                    for (int e = 0; e < kPiece; ++e) {
+                        const float a = y.a[e], b = y.b[e];
+                        y.a[e] = fmaf(a, z[e].c, b * z[e].s);
+                        y.b[e] = fmaf(b, z[e].c, -(a * z[e].s));
+                    }
                 }
-            }
-            if (live) {
-                u32x4 y0, y1;
-                pack<E, ADJ>(y, y0, y1);
-                E* p = static_cast<E*>(ho.p) + t * ho.token + (int64_t)r * ho.head;
-                *reinterpret_cast<u32x4*>(p + sp.e0) = y0;
-                *reinterpret_cast<u32x4*>(p + sp.e1) = y1;
+                if (g.norm) {
+                    const Piece x = unpack<E, ADJ>(x0[d], x1[d]);
+                    float q = 0.f, m = 0.f;
+#pragma unroll
+                    for (int e = 0; e < kPiece; ++e) {
+                        q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
+                        m = fmaf(y.a[e] * w.a[e], x.a[e], fmaf(y.b[e] * w.b[e], x.b[e], m));
+                    }
+                    q = group_sum<LP>(live ? q : 0.f);
+                    m = group_sum<LP>(live ? m : 0.f);
+                    const float n = 1.f / sqrtf(q / (float)g.dim + g.eps);
+                    m = m * n / (float)g.dim;
+#pragma unroll
+                    for (int e = 0; e < kPiece; ++e) {
+                        const float ua = x.a[e] * n, ub = x.b[e] * n;
+                        dw.a[e] += live ? y.a[e] * ua : 0.f;
+                        dw.b[e] += live ? y.b[e] * ub : 0.f;
+                        y.a[e] = n * fmaf(-ua, m, y.a[e] * w.a[e]);
+                        y.b[e] = n * fmaf(-ub, m, y.b[e] * w.b[e]);
+                    }
+                }
+                fetch(d, r + DEPTH * R);
+                if (live) {
+                    Raw<E> y0, y1;
+                    pack<E, ADJ>(y, y0, y1);
+                    E* p = static_cast<E*>(ho.p) + t * ho.token + (int64_t)r * ho.head;
+                    store(p + sp.e0, y0);
+                    store(p + sp.e1, y1);
+                }
             }
         }
     }
     if (!g.dw[kind]) return;   // the whole workgroup leaves together
 #pragma unroll
-    for (int e = 0; e < C; ++e) {
+    for (int e = 0; e < kPiece; ++e) {
         float a = dw.a[e], b = dw.b[e];
 #pragma unroll
         for (int m = LP; m < 64; m <<= 1) {
@@ -637,25 +627,24 @@ int back_groups(int cus) { return 4 * cus; }
 
 bool whole(const tr_heads& h, int eb)
 {
-    return ((uintptr_t)h.p | (uintptr_t)(h.token * eb) | (uintptr_t)(h.head * eb)) % 16 == 0;
+    return ((uintptr_t)h.p | (uintptr_t)(h.token * eb) | (uintptr_t)(h.head * eb)) % (kPiece * eb) == 0;
 }
 
-// Whether every head of the call is made of whole 16-byte pieces: its address,
-// its halves and its rotated part.
+// Whether every head of the call is made of whole pieces: its address, its
+// halves and its rotated part.
 bool in_pieces(const RotateArgs& a, int eb, bool back)
 {
-    const int two = 32 / eb;
-    if (a.dim % two || a.rot % two) return false;
+    if (a.dim % (2 * kPiece) || a.rot % (2 * kPiece)) return false;
     for (int k = 0; k < 3; ++k) {
         if (!a.heads[k]) continue;
         const bool to_cache = a.append && k > 0;
         if (!whole(a.in[k], eb) && !(back && !a.norm)) return false;
         if (!to_cache && !whole(a.out[k], eb)) return false;
         if (back && !whole(a.grad[k], eb)) return false;
-        if (k < 2 && (uintptr_t)a.w[k] % 16) return false;
+        if (k < 2 && (uintptr_t)a.w[k] % (kPiece * eb)) return false;
     }
-    return !a.append || ((((uintptr_t)a.cache.k | (uintptr_t)a.cache.v) % 16 == 0) &&
-                         ((a.cache.page | a.cache.token | a.cache.head) * eb) % 16 == 0);
+    return !a.append || ((((uintptr_t)a.cache.k | (uintptr_t)a.cache.v) % (kPiece * eb) == 0) &&
+                         (a.cache.page | a.cache.token | a.cache.head) % kPiece == 0);
 }
 
 template <typename E, int LP>
@@ -694,7 +683,7 @@ hipError_t rotate_typed(const RotateArgs& a, hipStream_t s)
         hipLaunchKernelGGL(rotate_any_kernel<E>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
         return hipGetLastError();
     }
-    const int lanes = a.dim * (int)sizeof(E) / 32;
+    const int lanes = a.dim / (2 * kPiece);
     if (lanes <= 4) return rotate_pieces<E, 4>(a, s);
     if (lanes <= 8) return rotate_pieces<E, 8>(a, s);
     if (lanes <= 16) return rotate_pieces<E, 16>(a, s);
@@ -712,7 +701,7 @@ hipError_t back_typed(const RotateArgs& a, hipStream_t s)
         hipLaunchKernelGGL(rotate_back_any_kernel<E>, dim3((unsigned)groups, 2), dim3(256), 0, s, a);
         e = hipGetLastError();
     } else {
-        const int lanes = a.dim * (int)sizeof(E) / 32;
+        const int lanes = a.dim / (2 * kPiece);
         e = lanes <= 4 ? back_pieces<E, 4>(a, groups, s) : lanes <= 8 ? back_pieces<E, 8>(a, groups, s)
             : lanes <= 16 ? back_pieces<E, 16>(a, groups, s) : back_pieces<E, 32>(a, groups, s);
     }
