@@ -37,13 +37,6 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float from_bf16(uint32_t v) { return __uint_as_float(v << 16); }
 
-// A value that is the same in all lanes, as a scalar.
-__device__ __forceinline__ int64_t uniform(int64_t x)
-{
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) |
-           (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
-}
-
 // Whether a word holds a bf16 that is not finite.
 __device__ __forceinline__ bool not_finite(uint32_t w)
 {

@@ -92,6 +92,13 @@ size_t attend_part_floats(int dim, int cus);
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
 
 // ---- device helpers ------------------------------------------------------------
+// A value that is the same in all lanes, as a scalar.
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
 // Sequence of packed row t: the last b with q_start[b] <= t, clamped to
 // [0, seqs - 1], by one wavefront (64 probes a step).
 __device__ __forceinline__ int sequence_of(const int32_t* q_start, int seqs, int64_t t, int lane)

@@ -121,6 +121,8 @@ tr_status check_tokens(const tr_attn* a, int64_t T)
 {
     if (!a) return fail(TR_EINVAL, "attn is NULL");
     if (T < 0 || T > kMaxTokens) return fail(TR_EINVAL, "T must be in [0, 2^31 - 1] (got %lld)", (long long)T);
+    if (T * (a->p.heads + 2 * (int64_t)a->p.kv_heads) > kMaxTokens - 65536)
+        return fail(TR_EUNSUPPORTED, "T = %lld tokens have more than 2^31 - 65536 heads", (long long)T);
     return TR_OK;
 }
 
@@ -406,8 +408,6 @@ tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const 
     if (window < 0 || (window > 0 && !causal))
         return fail(TR_EINVAL, "window must be >= 0, and 0 without causal (got %d)", window);
     if (T == 0) return TR_OK;
-    if (T * (a->p.heads / a->p.kv_heads) > kMaxTokens - 65536)
-        return fail(TR_EUNSUPPORTED, "T times the queries of a key head must stay below 2^31 - 65536");
     const int dim = a->p.head_dim;
     if ((st = check_cache(a, c, s)) != TR_OK || (st = check_heads("q", q, a->eb, T, a->p.heads)) != TR_OK ||
         (st = check_out_heads("out", out, a->eb, T, a->p.heads, dim)) != TR_OK)
