@@ -364,8 +364,6 @@ __device__ __forceinline__ void pack(const Piece& p, Raw<E>& x, Raw<E>& y)
 
 template <typename E>
 __device__ __forceinline__ Raw<E> load(const E* p) { return *reinterpret_cast<const Raw<E>*>(p); }
-template <typename E>
-__device__ __forceinline__ void store(E* p, Raw<E> v) { *reinterpret_cast<Raw<E>*>(p) = v; }
 
 // Sum over each group of LP lanes, the same bits in all of them.
 template <int LP>
@@ -553,15 +551,17 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int 
 // Gradients of one side (blockIdx.y): a wavefront walks over tokens t, t +
 // waves, ... and their heads, and keeps its lanes' share of dw, which a
 // workgroup joins into its row of `part`.
-template <typename E, int LP, bool ADJ>
+template <typename E, int LP, bool ADJ, bool STREAM>
 __global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
 {
     constexpr int R = 64 / LP, DEPTH = 2;
     __shared__ float red[4][kMaxHeadDim];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & (LP - 1), kind = blockIdx.y;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & (LP - 1), hl = lane / LP,
+              kind = blockIdx.y;
     const int rows = g.heads[kind];
     const int64_t waves = (int64_t)gridDim.x * 4;
     const Spot sp = spot_of<ADJ>(j, g.dim, g.rot);
+    const uint32_t b0 = sp.e0 * (uint32_t)sizeof(E), b1 = sp.e1 * (uint32_t)sizeof(E);
     const tr_heads hg = g.grad[kind], hx = g.in[kind], ho = g.out[kind];
     const Spin spin = spin_of(g, j, sp.turns);
     const float mean = 1.f / (float)g.dim;
@@ -571,29 +571,34 @@ __global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
     for (int e = 0; e < kPiece; ++e) dw.a[e] = dw.b[e] = 0.f;
     for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < g.tokens; t += waves) {
         Raw<E> g0[DEPTH], g1[DEPTH], x0[DEPTH], x1[DEPTH];
-        auto fetch = [&](int d, int r) {
-            if (r < rows && sp.on) {
-                const E* p = static_cast<const E*>(hg.p) + t * hg.token + (int64_t)r * hg.head;
-                g0[d] = load(p + sp.e0);
-                g1[d] = load(p + sp.e1);
+        auto fetch = [&](int d, int h) {              // heads h .. h + R - 1
+            if (h + hl < rows && sp.on) {
+                const char* p = static_cast<const char*>(hg.p) + (t * hg.token + (int64_t)h * hg.head) * (int)sizeof(E);
+                const uint32_t at = (uint32_t)hl * ((uint32_t)hg.head * (uint32_t)sizeof(E));
+                g0[d] = load(reinterpret_cast<const E*>(p + (at + b0)));
+                g1[d] = load(reinterpret_cast<const E*>(p + (at + b1)));
                 if (g.norm) {
-                    const E* q = static_cast<const E*>(hx.p) + t * hx.token + (int64_t)r * hx.head;
-                    x0[d] = load(q + sp.e0);
-                    x1[d] = load(q + sp.e1);
+                    const char* q = static_cast<const char*>(hx.p) + (t * hx.token + (int64_t)h * hx.head) * (int)sizeof(E);
+                    const uint32_t ax = (uint32_t)hl * ((uint32_t)hx.head * (uint32_t)sizeof(E));
+                    x0[d] = load(reinterpret_cast<const E*>(q + (ax + b0)));
+                    x1[d] = load(reinterpret_cast<const E*>(q + (ax + b1)));
                 }
             }
         };
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) fetch(d, d * R + lane / LP);
+        for (int d = 0; d < DEPTH; ++d) fetch(d, d * R);
         Turn z[kPiece];
         turns_of(g, spin, t, z);
-        for (int r0 = 0; r0 < rows; r0 += DEPTH * R) {
+        for (int h0 = 0; h0 < rows; h0 += DEPTH * R) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
-                if (r0 + d * R >= rows) break;
-                const int r = r0 + d * R + lane / LP;
-                const bool live = r < rows && sp.on;
+                const int h = h0 + d * R;
+                if (h >= rows) break;
+                const bool live = h + hl < rows && sp.on;
                 Piece y = unpack<E, ADJ>(g0[d], g1[d]);
+                [[maybe_unused]] Piece x;
+                if (g.norm) x = unpack<E, ADJ>(x0[d], x1[d]);
+                fetch(d, h + DEPTH * R);
                 if (sp.turns) {
 #pragma unroll
                     for (int e = 0; e < kPiece; ++e) {
@@ -603,7 +608,6 @@ __global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
                     }
                 }
                 if (g.norm) {
-                    const Piece x = unpack<E, ADJ>(x0[d], x1[d]);
                     float q = 0.f, m = 0.f;
 #pragma unroll
                     for (int e = 0; e < kPiece; ++e) {
@@ -623,13 +627,13 @@ __global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
                         y.b[e] = n * fmaf(-ub, m, y.b[e] * w.b[e]);
                     }
                 }
-                fetch(d, r + DEPTH * R);
                 if (live) {
                     Raw<E> y0, y1;
                     pack<E, ADJ>(y, y0, y1);
-                    E* p = static_cast<E*>(ho.p) + t * ho.token + (int64_t)r * ho.head;
-                    store(p + sp.e0, y0);
-                    store(p + sp.e1, y1);
+                    char* p = static_cast<char*>(ho.p) + (t * ho.token + (int64_t)h * ho.head) * (int)sizeof(E);
+                    const uint32_t at = (uint32_t)hl * ((uint32_t)ho.head * (uint32_t)sizeof(E));
+                    put<STREAM>(reinterpret_cast<E*>(p + (at + b0)), y0);
+                    put<STREAM>(reinterpret_cast<E*>(p + (at + b1)), y1);
                 }
             }
         }
@@ -654,7 +658,10 @@ __global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
 }
 
 // ---- launches ------------------------------------------------------------------------
-int back_groups(int cus) { return 4 * cus; }
+// Workgroups of a side: with both sides' the chip is full at once, and each
+// wavefront walks over many tokens (16384 tokens of 40 bf16 heads of 128: 102 us
+// with two a CU, 112 with four, 121 with eight).
+int back_groups(int cus) { return 2 * cus; }
 
 bool whole(const tr_heads& h, int eb)
 {
@@ -719,7 +726,9 @@ hipError_t back_pieces(const RotateArgs& a, int groups, hipStream_t s)
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups, 2), dim3(256), 0, s, a);
         return hipGetLastError();
     };
-    return a.adjacent ? launch(rotate_back_kernel<E, LP, true>) : launch(rotate_back_kernel<E, LP, false>);
+    const bool stream = a.tokens * (a.heads[0] + a.heads[1]) * a.dim * (int64_t)sizeof(E) >= kStreamBytes;
+    if (stream) return a.adjacent ? launch(rotate_back_kernel<E, LP, true, true>) : launch(rotate_back_kernel<E, LP, false, true>);
+    return a.adjacent ? launch(rotate_back_kernel<E, LP, true, false>) : launch(rotate_back_kernel<E, LP, false, false>);
 }
 
 template <typename E>
