@@ -37,6 +37,23 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float from_bf16(uint32_t v) { return __uint_as_float(v << 16); }
 
+// The largest of three, numbers before NaN, in one instruction (fmaxf of a matrix
+// instruction's result first quiets it in another).
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+
+// Two values rounded to bf16, the first one low.
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y)
+{
+    uint32_t r;
+    asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+    return r;
+}
+
 // Whether a word holds a bf16 that is not finite.
 __device__ __forceinline__ bool not_finite(uint32_t w)
 {
@@ -372,13 +389,14 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
             const float keep = exp2_(m - zero);
             m = m1;
             l *= keep;
-            s16x8 pb;
+            u32x4 pb;
 #pragma unroll
             for (int v = 0; v < 8; ++v) {
                 p[v] = exp2_(p[v] - zero);
                 l += p[v];
-                pb[v] = (short)to_bf16(p[v]);
             }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) pb[v] = pack_bf16(p[2 * v], p[2 * v + 1]);
             if (!__all(keep == 1.f)) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= keep;
@@ -389,9 +407,11 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
                 // key, and count as zeros in the product
 #pragma unroll 1
                 for (int i = 0; i < kTile; ++i) {
-                    const uint32_t w01 = i & 1 ? (uint16_t)pb[1] : (uint16_t)pb[0], w23 = i & 1 ? (uint16_t)pb[3] : (uint16_t)pb[2];
-                    const uint32_t w45 = i & 1 ? (uint16_t)pb[5] : (uint16_t)pb[4], w67 = i & 1 ? (uint16_t)pb[7] : (uint16_t)pb[6];
-                    const float w = from_bf16(__shfl(i & 16 ? (i & 2 ? w67 : w45) : (i & 2 ? w23 : w01), (i & 12) * 4 + col));
+                    uint32_t y = 0;       // key i lies in group (i / 4) % 4, element 4 (i / 16) + i % 4
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) y = v == (i >> 4) * 2 + (i >> 1 & 1) ? pb[v] : y;
+                    y = __shfl(y, (i & 12) * 4 + col);
+                    const float w = from_bf16(i & 1 ? y >> 16 : y & 0xffffu);
                     const bool sees = j0 + i >= lo && j0 + i < hi;
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
@@ -557,6 +577,12 @@ __device__ __forceinline__ void load_lds(uint32_t lds, const void* p)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
 
+// The same from base + off, the base the wavefront's.
+__device__ __forceinline__ void load_lds(uint32_t lds, const void* base, uint32_t off)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+
 __device__ __forceinline__ void wait_all_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ float max_halves(float x)
@@ -565,13 +591,16 @@ __device__ __forceinline__ float max_halves(float x)
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int DH, int NW, int STEP, bool FULL>
+// PG16: pages of whole 16 tokens, below 2 GB: the rows that one wavefront's load
+// fills lie in one page, whose address is the wavefront's.
+template <int DH, int NW, int STEP, bool PG16, bool FULL>
 __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel(AttendArgs a)
 {
     constexpr int ROWS = NW * kManyRows, T = NW * 64;
     constexpr int KF = DH / 16, DT = DH / 32;               // fragments of keys, tiles of elements
     constexpr int PIECES = DH / 8, BYTES = kManyTile * DH * 2;
     constexpr int LR = T / PIECES, NI = kManyTile / LR;     // rows of one round of loads, rounds of a tile
+    constexpr int WR = 64 / PIECES;                         // rows that a wavefront loads
     __shared__ __align__(16) unsigned char smem[4 * BYTES]; // stage 0: K, V; stage 1: K, V
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
@@ -646,26 +675,40 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
         const int32_t* table = a.step.table + (int64_t)pl.b * a.step.table_stride;
         const uint16_t* kp = static_cast<const uint16_t*>(a.cache.k) + (int64_t)h * a.cache.head;
         const uint16_t* vp = static_cast<const uint16_t*>(a.cache.v) + (int64_t)h * a.cache.head;
+        // Rows that no row of the tile sees are read as the nearest that one does.
         int page[NI], in[NI];
         auto pages = [&](int j) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                // rows that no row of the tile sees are read as the nearest that one does
-                const int t = min(max(j + i * LR + lrow, lo_min), last);
-                const int slot = (int)divide((uint32_t)t, a.by_page);
-                page[i] = table[slot];
-                in[i] = t - slot * a.cache.page_size;
+                if constexpr (PG16) {
+                    const int t0 = min(max(j + i * LR + wave * WR, lo_min & ~15), last & ~15) & ~15;
+                    const int slot = (int)divide((uint32_t)t0, a.by_page);
+                    page[i] = table[slot];
+                    in[i] = min(max(j + i * LR + lrow, lo_min), last) - slot * a.cache.page_size;
+                } else {
+                    const int t = min(max(j + i * LR + lrow, lo_min), last);
+                    const int slot = (int)divide((uint32_t)t, a.by_page);
+                    page[i] = table[slot];
+                    in[i] = t - slot * a.cache.page_size;
+                }
             }
         };
         auto load = [&](int stage) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const int row = i * LR + lrow;
-                const int64_t at = (int64_t)min(max(page[i], 0), a.cache.pages - 1) * a.cache.page + (int64_t)in[i] * a.cache.token;
                 const int kc = (lpos ^ k_swizzle<DH>(row)) * 8, vc = (lpos ^ v_swizzle<DH>(row)) * 8;
                 const uint32_t to = lds0 + stage * 2 * BYTES + (i * T + wave * 64) * 16;
-                if (FULL || kc < a.dim) load_lds(to, kp + at + kc);
-                if (FULL || vc < a.dim) load_lds(to + BYTES, vp + at + vc);
+                if constexpr (PG16) {
+                    const int64_t at = (int64_t)min(max(__builtin_amdgcn_readfirstlane(page[i]), 0), a.cache.pages - 1) * a.cache.page;
+                    const uint32_t off = (uint32_t)in[i] * (uint32_t)(a.cache.token * 2);
+                    if (FULL || kc < a.dim) load_lds(to, kp + at, off + kc * 2);
+                    if (FULL || vc < a.dim) load_lds(to + BYTES, vp + at, off + vc * 2);
+                } else {
+                    const int64_t at = (int64_t)min(max(page[i], 0), a.cache.pages - 1) * a.cache.page + (int64_t)in[i] * a.cache.token;
+                    if (FULL || kc < a.dim) load_lds(to, kp + at + kc);
+                    if (FULL || vc < a.dim) load_lds(to + BYTES, vp + at + vc);
+                }
             }
         };
         if (j0 < j_end) {
@@ -712,6 +755,7 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
                 }
             }
             if (!full_rows || j0 < wlo_max || j0 + kManyTile > whi_min) {
+                asm volatile("");      // a branch: most tiles need none of this
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -722,7 +766,7 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
             }
             float top = minus_inf();
 #pragma unroll
-            for (int v = 0; v < 16; ++v) top = fmaxf(top, fmaxf(sc[0][v], sc[1][v]));
+            for (int v = 0; v < 16; ++v) top = max3(top, sc[0][v], sc[1][v]);
             top = max_halves(top);
             // The maximum that a row's weights are relative to follows only when it is
             // left behind by 2^8: sums scaled by less than that lose nothing.
@@ -735,15 +779,18 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
                 for (int d = 0; d < DT; ++d) o[d] *= keep;
             }
             const float zero = m == minus_inf() ? 0.f : m * a.scale;
-            s16x8 pb[4];
+            u32x4 pb[4];
+            float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const float p = exp2_(fmaf(sc[x][v], a.scale, -zero));
-                    l += p;
-                    pb[2 * x + v / 8][v % 8] = (short)to_bf16(p);
+                for (int v = 0; v < 16; v += 2) {
+                    const float p = exp2_(fmaf(sc[x][v], a.scale, -zero)), q = exp2_(fmaf(sc[x][v + 1], a.scale, -zero));
+                    sum[0] += p;
+                    sum[1] += q;
+                    pb[2 * x + v / 8][v / 2 % 4] = pack_bf16(p, q);
                 }
+            l += sum[0] + sum[1];
             if (bad) {
                 // such values go to the rows that see them, key by key, and count as
                 // zeros in the product
@@ -754,9 +801,9 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
 #pragma unroll
-                        for (int v = 0; v < 8; ++v)
-                            w = x == i >> 4 && v == (i >> 3 & 1) * 4 + (i & 3) ? (uint32_t)(uint16_t)pb[x][v] : w;
-                    const float p = from_bf16(__shfl(w, (i & 4) * 8 + col));
+                        for (int v = 0; v < 4; ++v) w = x == i >> 4 && v == (i >> 3 & 1) * 2 + (i >> 1 & 1) ? pb[x][v] : w;
+                    w = __shfl(w, (i & 4) * 8 + col);
+                    const float p = from_bf16(i & 1 ? w >> 16 : w & 0xffffu);
                     const bool sees = j0 + i >= lo && j0 + i < hi;
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
@@ -837,11 +884,17 @@ Divisor divisor(uint32_t d)
     return v;
 }
 
+// Whether 16 tokens from a multiple of 16 on lie in one page of less than 2 GB.
+bool in_halves(const AttendArgs& a)
+{
+    return a.cache.page_size % 16 == 0 && a.cache.token < INT32_MAX / 2 && a.cache.token * 2 * (int64_t)a.cache.page_size < INT32_MAX;
+}
+
 template <int DH>
 hipError_t few(const AttendArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)(kFewPerCu<DH> * a.cus));
-    const bool pg16 = a.cache.page_size % 16 == 0 && a.cache.token * 2 * (int64_t)a.cache.page_size < INT32_MAX;
+    const bool pg16 = in_halves(a);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(kFewThreads), 0, s, a);
         return hipGetLastError();
@@ -869,9 +922,16 @@ hipError_t many(const AttendArgs& a, hipStream_t s)
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(NW * 64), 0, s, a);
         return hipGetLastError();
     };
-    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus)
-        return a.dim == DH ? launch(attend_many_kernel<DH, NW, 0, true>, items) : launch(attend_many_kernel<DH, NW, 0, false>, items);
-    hipError_t e = a.dim == DH ? launch(attend_many_kernel<DH, NW, kManyStep, true>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false>, a.cus);
+    const bool pg16 = in_halves(a);
+    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus) {
+        if (a.dim == DH) return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, true>, items) : launch(attend_many_kernel<DH, NW, 0, false, true>, items);
+        return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, false>, items) : launch(attend_many_kernel<DH, NW, 0, false, false>, items);
+    }
+    hipError_t e;
+    if (a.dim == DH)
+        e = pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, true>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, true>, a.cus);
+    else
+        e = pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, false>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, false>, a.cus);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((join_kernel<DH, ROWS, kManyStep>), dim3((unsigned)a.cus, ROWS / 16), dim3(1024), 0, s, a);
     return hipGetLastError();
