@@ -14,6 +14,8 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
+from itertools import chain
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
@@ -21,12 +23,18 @@ import torch
 from . import _lib
 from ._lib import AttnParams, Cache, Heads, StepArgs
 
+# Small calls are bound by this module's own work (one decoded token: 9 us a call
+# against 15 us on the device), so each tensor is looked at once, devices are
+# compared as indices, and streams are asked for as plain handles.
+
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") \
+    else lambda index: torch.cuda.current_stream(index).cuda_stream
 _DTYPES = {torch.float32: _lib.TR_FP32, torch.bfloat16: _lib.TR_BF16}
 _NONE = Heads(None, 0, 0)
 
 
 def _check(status: int, where: str):
-    if status != _lib.TR_OK:
+    if status:
         from . import TRError
         raise TRError(status, where)
 
@@ -70,33 +78,43 @@ def kept_positions(idx: torch.Tensor, K: Sequence[int], grid: Sequence[Tuple[int
     columns (a prompt's text) stay as they are.
     """
     lib = _lib.load()
-    B, kept = len(K), sum(map(int, K))
-    if not idx.is_cuda or idx.dtype != torch.int32 or idx.dim() != 1 or not idx.is_contiguous() or idx.numel() != kept:
+    B = len(K)
+    counts = array("i", K)
+    kept = sum(counts)
+    if not isinstance(idx, torch.Tensor) or not idx.is_cuda or idx.dtype is not torch.int32 or idx.dim() != 1 \
+            or not idx.is_contiguous() or idx.numel() != kept:
         raise ValueError("idx must be a contiguous int32 [sum K] tensor on a ROCm device")
     if len(grid) != B or len(start) != B or (dst is not None and len(dst) != B):
         raise ValueError("grid, start and dst must have one entry for each image")
-    if any(len(g) != 3 for g in grid) or any(len(s) != 3 for s in start):
+    if B and (set(map(len, grid)) != {3} or set(map(len, start)) != {3}):
         raise ValueError("entries of grid and start must be (time, height, width)")
-    if dst is not None and out is None:
-        raise ValueError("dst needs out")
     if out is None:
+        if dst is not None:
+            raise ValueError("dst needs out")
         out = _empty((3, kept), torch.int32, idx.device, stream)
-    elif out.device != idx.device or out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 \
+    elif out.device != idx.device or out.dtype is not torch.int32 or out.dim() != 2 or out.shape[0] != 3 \
             or (out.shape[1] > 1 and out.stride(1) != 1):
         raise ValueError("out must be an int32 [3, columns] tensor with unit column stride on %s" % idx.device)
     elif out.shape[1] and out.stride(0) < out.shape[1]:
         raise ValueError("out has rows that overlap")
-    i32 = ctypes.c_int32
-    flat = (i32 * (3 * B))(*[int(x) for g in grid for x in g])
-    first = (i32 * (3 * B))(*[int(x) for s in start for x in s])
-    to = None if dst is None else (ctypes.c_int64 * B)(*map(int, dst))
-    if dst is not None and any(int(d) < 0 or int(d) + int(k) > out.shape[1] for d, k in zip(dst, K)) \
-            or dst is None and kept > out.shape[1]:
+    columns = out.shape[1]
+    to = None if dst is None else array("q", dst)
+    if to is None:
+        if kept > columns:
+            raise ValueError("the images' columns do not fit out")
+    elif any(d < 0 or d + k > columns for d, k in zip(to, counts)):
         raise ValueError("the images' columns do not fit out")
-    st = stream if stream is not None else torch.cuda.current_stream(idx.device)
-    with torch.cuda.device(idx.device):
-        _check(lib.tr_kept_positions(_ptr(idx), B, (i32 * B)(*map(int, K)), flat, first, to, _ptr(out),
-                                     out.stride(0) if out.shape[1] else 0, st.cuda_stream), "tr_kept_positions")
+    shape, first = array("i", chain.from_iterable(grid)), array("i", chain.from_iterable(start))
+    args = (idx.data_ptr(), B, counts.buffer_info()[0], shape.buffer_info()[0], first.buffer_info()[0],
+            None if to is None else to.buffer_info()[0], out.data_ptr(), out.stride(0) if columns else 0)
+    index = idx.get_device()
+    handle = _raw_stream(index) if stream is None else stream.cuda_stream
+    if index == torch.cuda.current_device():
+        status = lib.tr_kept_positions(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            status = lib.tr_kept_positions(*args, handle)
+    _check(status, "tr_kept_positions")
     return out
 
 
@@ -140,6 +158,7 @@ class Attention:
             raise RuntimeError("paper_2607_13500_amd needs a ROCm GPU (gfx950)")
         self.device = torch.device("cuda", torch.cuda.current_device() if device is None
                                    else torch.device(device).index or 0)
+        self._index = self.device.index
         self.lib = _lib.load()
         freq = None if inv_freq is None else (ctypes.c_double * max(pairs, 1))(*map(float, inv_freq))
         axis = None if pair_axis is None else (ctypes.c_int32 * max(pairs, 1))(*map(int, pair_axis))
@@ -154,64 +173,71 @@ class Attention:
 
     # -- helpers ----------------------------------------------------------
     def _stream(self, stream):
-        st = stream if stream is not None else torch.cuda.current_stream(self.device)
-        return st.cuda_stream
+        return _raw_stream(self._index) if stream is None else stream.cuda_stream
 
-    def _heads(self, name, t, heads, tokens=None) -> Heads:
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+    def _heads(self, name, t, heads, tokens) -> Heads:
+        if not isinstance(t, torch.Tensor) or t.get_device() != self._index:
             raise ValueError("%s must be a tensor on %s" % (name, self.device))
-        if t.dtype != self.dtype:
+        if t.dtype is not self.dtype:
             raise TypeError("%s must be %s, got %s" % (name, self.dtype, t.dtype))
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim \
-                or (tokens is not None and t.shape[0] != tokens) or (self.head_dim > 1 and t.stride(2) != 1):
-            raise ValueError("%s must be a [%s, %d, %d] tensor with unit element stride, got %s of strides %s"
-                             % (name, "tokens" if tokens is None else tokens, heads, self.head_dim, tuple(t.shape), t.stride()))
-        return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+        if t.shape == (tokens, heads, self.head_dim):
+            token, head, unit = t.stride()
+            if unit == 1 or self.head_dim == 1:
+                return Heads(t.data_ptr(), token, head)
+        raise ValueError("%s must be a [%s, %d, %d] tensor with unit element stride, got %s of strides %s"
+                         % (name, tokens, heads, self.head_dim, tuple(t.shape), t.stride()))
 
     def _out(self, name, t, tokens, heads, stream):
         if t is None:
-            t = _empty((tokens, heads, self.head_dim), self.dtype, self.device, stream)
+            dim = self.head_dim
+            t = _empty((tokens, heads, dim), self.dtype, self.device, stream)
+            return t, Heads(t.data_ptr(), heads * dim, dim)
         return t, self._heads(name, t, heads, tokens)
 
     def _pos(self, pos, tokens):
-        if not isinstance(pos, torch.Tensor) or pos.device != self.device or pos.dtype != torch.int32:
+        if not isinstance(pos, torch.Tensor) or pos.get_device() != self._index or pos.dtype is not torch.int32:
             raise ValueError("pos must be an int32 tensor on %s" % self.device)
         if pos.dim() == 1 and self.axes == 1:
             pos = pos[None]
-        if pos.dim() != 2 or pos.shape[0] != self.axes or pos.shape[1] != tokens \
-                or (tokens > 1 and pos.stride(1) != 1) or (self.axes > 1 and pos.stride(0) < tokens):
-            raise ValueError("pos must be [%d, %d] with unit column stride, got %s" % (self.axes, tokens, tuple(pos.shape)))
-        return pos.data_ptr(), max(pos.stride(0), tokens)
+        if pos.shape == (self.axes, tokens):
+            row, unit = pos.stride()
+            if (unit == 1 or tokens <= 1) and (row >= tokens or self.axes == 1):
+                return pos.data_ptr(), max(row, tokens)
+        raise ValueError("pos must be [%d, %d] with unit column stride, got %s" % (self.axes, tokens, tuple(pos.shape)))
 
     def _weight(self, name, w):
-        if w is not None and (not isinstance(w, torch.Tensor) or w.device != self.device or w.dtype != self.dtype
-                              or tuple(w.shape) != (self.head_dim,) or not w.is_contiguous()):
+        if w is None:
+            return None
+        if not isinstance(w, torch.Tensor) or w.get_device() != self._index or w.dtype is not self.dtype \
+                or w.shape != (self.head_dim,) or not w.is_contiguous():
             raise ValueError("%s must be a contiguous %s [%d] tensor on %s" % (name, self.dtype, self.head_dim, self.device))
-        return _ptr(w)
+        return w.data_ptr()
 
     def _cache(self, cache: KVCache) -> Cache:
         k, v = cache
         for name, t in (("cache.k", k), ("cache.v", v)):
-            if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype:
+            if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype is not self.dtype:
                 raise ValueError("%s must be a %s tensor on %s" % (name, self.dtype, self.device))
-            if t.dim() != 4 or tuple(t.shape[2:]) != (self.kv_heads, self.head_dim) or (self.head_dim > 1 and t.stride(3) != 1):
-                raise ValueError("%s must be [pages, page_size, %d, %d] with unit element stride, got %s"
-                                 % (name, self.kv_heads, self.head_dim, tuple(t.shape)))
-        if k.shape != v.shape or k.stride() != v.stride():
+        shape, stride = k.shape, k.stride()
+        if len(shape) != 4 or shape[2] != self.kv_heads or shape[3] != self.head_dim or (self.head_dim > 1 and stride[3] != 1):
+            raise ValueError("cache.k must be [pages, page_size, %d, %d] with unit element stride, got %s of strides %s"
+                             % (self.kv_heads, self.head_dim, tuple(shape), stride))
+        if shape != v.shape or stride != v.stride():
             raise ValueError("cache.k and cache.v must have the same shape and strides")
-        return Cache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1], k.stride(0), k.stride(1), k.stride(2))
+        return Cache(k.data_ptr(), v.data_ptr(), shape[0], shape[1], stride[0], stride[1], stride[2])
 
     def _step(self, step: Step) -> StepArgs:
+        for name, t in zip(Step._fields, step):
+            if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype is not torch.int32:
+                raise ValueError("step.%s must be an int32 tensor on %s" % (name, self.device))
         q_start, kv_len, table = step
-        for name, t, dim in (("q_start", q_start, 1), ("kv_len", kv_len, 1), ("table", table, 2)):
-            if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != torch.int32 or t.dim() != dim:
-                raise ValueError("step.%s must be an int32 tensor of %d dimensions on %s" % (name, dim, self.device))
-        seqs = kv_len.numel()
-        if q_start.numel() != seqs + 1 or table.shape[0] != seqs or not q_start.is_contiguous() \
-                or not kv_len.is_contiguous() or (table.shape[1] > 1 and table.stride(1) != 1):
-            raise ValueError("step must hold q_start [seqs + 1], kv_len [seqs] and table [seqs, width], rows contiguous")
-        return StepArgs(seqs, table.shape[1], max(table.stride(0), table.shape[1]) if seqs == 1 else table.stride(0),
-                        q_start.data_ptr(), kv_len.data_ptr(), table.data_ptr())
+        if kv_len.dim() == 1 and table.dim() == 2:
+            seqs, (rows, width), (row, unit) = kv_len.shape[0], table.shape, table.stride()
+            if q_start.shape == (seqs + 1,) and rows == seqs and (unit == 1 or width <= 1) and q_start.is_contiguous() \
+                    and kv_len.is_contiguous():
+                return StepArgs(seqs, width, row if seqs > 1 else max(row, width), q_start.data_ptr(), kv_len.data_ptr(),
+                                table.data_ptr())
+        raise ValueError("step must hold q_start [seqs + 1], kv_len [seqs] and table [seqs, width], rows contiguous")
 
     # -- the operators ------------------------------------------------------
     def rotate(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: torch.Tensor, *,
@@ -277,9 +303,9 @@ class Attention:
             hq = self._heads("q", q, self.heads, tokens)
             q_out, oq = self._out("q_out", q_out, tokens, self.heads, stream)
         at, ldpos = self._pos(pos, tokens)
-        c, s = self._cache(cache), self._step(step)
-        _check(self.lib.tr_append(self._ctx, tokens, hq, hk, hv, self._weight("wq", wq), self._weight("wk", wk), at,
-                                  ldpos, oq, ctypes.byref(c), ctypes.byref(s), self._stream(stream)), "tr_append")
+        status = self.lib.tr_append(self._ctx, tokens, hq, hk, hv, self._weight("wq", wq), self._weight("wk", wk), at,
+                                    ldpos, oq, self._cache(cache), self._step(step), self._stream(stream))
+        _check(status, "tr_append")
         return q_out if q is not None else None
 
     def attend(self, q: torch.Tensor, cache: KVCache, step: Step, *, scale: Optional[float] = None,
@@ -298,10 +324,10 @@ class Attention:
         hq = self._heads("q", q, self.heads, tokens)
         out, ho = self._out("out", out, tokens, self.heads, stream)
         lse = _empty((tokens, self.heads), torch.float32, self.device, stream) if want_lse else None
-        c, s = self._cache(cache), self._step(step)
-        _check(self.lib.tr_attend(self._ctx, tokens, hq, ctypes.byref(c), ctypes.byref(s),
-                                  1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(bool(causal)),
-                                  int(window), ho, _ptr(lse), self._stream(stream)), "tr_attend")
+        status = self.lib.tr_attend(self._ctx, tokens, hq, self._cache(cache), self._step(step),
+                                    1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), 1 if causal else 0,
+                                    int(window), ho, _ptr(lse), self._stream(stream))
+        _check(status, "tr_attend")
         return out, lse
 
     def close(self):
