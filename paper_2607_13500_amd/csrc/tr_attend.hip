@@ -98,8 +98,8 @@ __device__ __forceinline__ void seen_by(const AttendArgs& a, const Sequence& s, 
 // The work is the items (sequence, key head, tile of 16 rows), each with its
 // range of keys in steps of kStep.  All steps of all items in a row are dealt
 // out to the workgroups in equal shares, whatever the sequences' lengths: a
-// workgroup's share can end inside an item, and then the item's parts are joined
-// by join_kernel.  A workgroup's four wavefronts take tiles of 32 keys in turn,
+// workgroup's share can end inside an item, and then the last of its workgroups
+// to arrive joins the item's parts.  A workgroup's four wavefronts take tiles of 32 keys in turn,
 // each with its own maximum and sums, and join them at the end of an item.
 //
 // Bound by the bytes of the cache: a wavefront has the next tile's keys and
@@ -140,14 +140,38 @@ __device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b)
     return (int64_t)tiles_of<ROWS>(a, s) * steps_of<STEP>(s) * a.kv_heads;
 }
 
+// All steps, and a workgroup's share of them.  An item has at most kMostParts
+// parts, which one workgroup can join.
+constexpr int kMostParts = 64;
+
+struct Shares {
+    int64_t total, share;
+};
+
 template <int ROWS, int STEP>
-__device__ __forceinline__ int64_t all_steps(const AttendArgs& a, int lane)
+__device__ __forceinline__ Shares shares_of(const AttendArgs& a, int lane)
 {
     int64_t sum = 0;
-    for (int b0 = 0; b0 < a.step.seqs; b0 += 64) sum += cost_of<ROWS, STEP>(a, b0 + lane);
+    int most = 0;
+    for (int b0 = 0; b0 < a.step.seqs; b0 += 64) {
+        const int b = b0 + lane;
+        if (b < a.step.seqs) {
+            const Sequence s = sequence_at(a, b);
+            const int steps = steps_of<STEP>(s);
+            sum += (int64_t)tiles_of<ROWS>(a, s) * steps * a.kv_heads;
+            most = max(most, steps);
+        }
+    }
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
-    return uniform(sum);
+    for (int m = 1; m < 64; m <<= 1) {
+        sum += __shfl_xor(sum, m);
+        most = max(most, __shfl_xor(most, m));
+    }
+    Shares r;
+    r.total = uniform(sum);
+    r.share = max((r.total + gridDim.x - 1) / gridDim.x,
+                  (int64_t)((__builtin_amdgcn_readfirstlane(most) + kMostParts - 1) / kMostParts));
+    return r;
 }
 
 // The sequence that step u (< all_steps) lies in.
@@ -203,9 +227,72 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, int64_t t, int h
     if (a.lse && e0 == 0) a.lse[t * a.heads + head] = some ? fmaf(m, kLn2, __logf(l)) : minus_inf();
 }
 
-// Floats of one part in the scratch: ROWS rows of DH sums, their maxima and l.
+// ---- parts of items ------------------------------------------------------------------
+// A part that another workgroup, on another XCD, is to read is written and read
+// past the L2s, by accesses of agent scope.  A workgroup's two parts are the end
+// of an item begun before it (0) and the beginning of one that goes on past it (1).
+__device__ __forceinline__ void put2(float* p, float x, float y)
+{
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x),
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ float2 get2(const float* p)
+{
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return float2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+
+// Floats of a part: ROWS rows of DH sums, their maxima and l.
 template <int DH, int ROWS>
 constexpr int kPartFloats = ROWS * DH + 2 * ROWS;
+
+// One item's parts: `count` of them, this workgroup's is number `mine`, the
+// first is workgroup `owner`'s second.
+struct Parts {
+    int owner, count, mine;
+};
+
+__device__ __forceinline__ Parts parts_of(int64_t begin, int64_t end, int64_t share)
+{
+    Parts p;
+    p.owner = (int)(begin / share);
+    p.count = (int)((end - 1) / share) - p.owner + 1;
+    p.mine = (int)blockIdx.x - p.owner;
+    return p;
+}
+
+template <int FLOATS>
+__device__ __forceinline__ float* part_at(const AttendArgs& a, const Parts& p, int i)
+{
+    return a.part + ((int64_t)(p.owner + i) * 2 + (i == 0)) * FLOATS;
+}
+
+// Whether all other parts are there already; the same in the whole workgroup.
+__device__ __forceinline__ bool others_done(const AttendArgs& a, const Parts& p, int* shared)
+{
+    if (threadIdx.x == 0)
+        *shared = __hip_atomic_load(a.arrived + p.owner, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.count - 1;
+    __syncthreads();
+    return *shared != 0;
+}
+
+// After this workgroup's part is written: whether it was the last one.
+__device__ __forceinline__ bool last_to_arrive(const AttendArgs& a, const Parts& p, int* shared)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's stores are done
+    __syncthreads();
+    if (threadIdx.x == 0)
+        *shared = __hip_atomic_fetch_add(a.arrived + p.owner, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.count - 1;
+    __syncthreads();
+    return *shared != 0;
+}
+
+// The count is back at zero for the next call.
+__device__ __forceinline__ void joined(const AttendArgs& a, const Parts& p)
+{
+    if (threadIdx.x == 0) __hip_atomic_store(a.arrived + p.owner, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 // Address swizzle of a row of V in shared memory, in pieces of 16 bytes: the 16
 // rows that a transposing read touches spread over all banks.
@@ -231,6 +318,7 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
     constexpr int kLds = 4 * (kTile * DH * 2 > kRows * PAD * 4 ? kTile * DH * 2 : kRows * PAD * 4);
     __shared__ __align__(16) unsigned char smem[kLds];
     __shared__ float ml[4][2][kRows];
+    __shared__ int flag;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
@@ -239,10 +327,9 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
     const int token_bytes = (int)(a.cache.token * 2);            // PG16
     const int k_lane = col * token_bytes + grp * 16, v_lane = vrow * token_bytes + piece * 16;
 
-    const int64_t total = all_steps<kRows, kStep>(a, lane);
-    const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
-    int64_t u = (int64_t)blockIdx.x * share;
-    const int64_t u_end = min(u + share, total);
+    const Shares all = shares_of<kRows, kStep>(a, lane);
+    int64_t u = (int64_t)blockIdx.x * all.share;
+    const int64_t u_end = min(u + all.share, all.total);
 
     while (u < u_end) {
         const Place pl = place_of<kRows, kStep>(a, u, lane);
@@ -475,73 +562,59 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
 #pragma unroll
                 for (int e = 0; e < N; ++e) acc[e] = fmaf(red[(w * kRows + row) * PAD + e0 + e], f, acc[e]);
             }
-            if (row < rows) {
-                if (whole) {
-                    const uint32_t rr = (uint32_t)(rt * kRows + row);
-                    const int t = (int)divide(rr, a.by_group), hd = h * a.group + (int)(rr - (uint32_t)t * a.group);
-                    finish_row<N>(a, s.q0 + t, hd, e0, acc, sum, top);
-                } else {
-                    float* part = a.part + ((int64_t)blockIdx.x * 2 + (step0 == 0)) * kPartFloats<DH, kRows>;
+            const uint32_t rr = (uint32_t)(rt * kRows + row);
+            const int t = (int)divide(rr, a.by_group), hd = h * a.group + (int)(rr - (uint32_t)t * a.group);
+            bool finish = whole;
+            if (!whole) {
+                constexpr int F = kPartFloats<DH, kRows>;
+                const int64_t begin = pl.first + (int64_t)item * pl.steps;
+                const Parts parts = parts_of(begin, begin + pl.steps, all.share);
+                float* part = part_at<F>(a, parts, parts.mine);
+                if (row < rows) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) part[row * DH + e0 + e] = acc[e];
-                    if (e0 == 0) {
-                        part[kRows * DH + row] = top;
-                        part[kRows * DH + kRows + row] = sum;
+                    for (int e = 0; e < N; e += 2) put2(part + row * DH + e0 + e, acc[e], acc[e + 1]);
+                    if (e0 == 0) put2(part + kRows * DH + 2 * row, top, sum);
+                }
+                finish = last_to_arrive(a, parts, &flag);
+                if (finish) {
+                    // all parts in their order, eight of them on their way at a time
+                    constexpr int U = N > 8 ? 4 : 8;
+                    if (row < rows) {
+                        top = minus_inf();
+                        sum = 0.f;
+#pragma unroll
+                        for (int e = 0; e < N; ++e) acc[e] = 0.f;
+                        for (int i0 = 0; i0 < parts.count; i0 += U) {
+                            float2 ml_i[U], v[U][N / 2];
+#pragma unroll
+                            for (int i = 0; i < U; ++i) {
+                                const float* q = part_at<F>(a, parts, min(i0 + i, parts.count - 1));
+                                ml_i[i] = get2(q + kRows * DH + 2 * row);
+#pragma unroll
+                                for (int e = 0; e < N; e += 2) v[i][e / 2] = get2(q + row * DH + e0 + e);
+                            }
+#pragma unroll
+                            for (int i = 0; i < U; ++i) {
+                                if (i0 + i >= parts.count) break;
+                                const float m1 = fmaxf(top, ml_i[i].x), z = m1 == minus_inf() ? 0.f : m1;
+                                const float f = exp2_(top - z), g = exp2_(ml_i[i].x - z);
+                                top = m1;
+                                sum = fmaf(ml_i[i].y, g, sum * f);
+#pragma unroll
+                                for (int e = 0; e < N; e += 2) {
+                                    acc[e] = fmaf(v[i][e / 2].x, g, acc[e] * f);
+                                    acc[e + 1] = fmaf(v[i][e / 2].y, g, acc[e + 1] * f);
+                                }
+                            }
+                        }
                     }
+                    joined(a, parts);
                 }
             }
+            if (finish && row < rows) finish_row<N>(a, s.q0 + t, hd, e0, acc, sum, top);
         }
         __syncthreads();
         u += step1 - step0;
-    }
-}
-
-// Joins the parts of each item that several workgroups worked on: workgroup i
-// does the item that began in workgroup i of the kernel before (of `groups`)
-// and went on past it, whose later parts are the first ones of the workgroups
-// after i.  One wavefront a row, 16 rows of the item to a workgroup.
-template <int DH, int ROWS, int STEP>
-__global__ __launch_bounds__(1024) void join_kernel(AttendArgs a)
-{
-    constexpr int N = DH / 64;
-    const int lane = threadIdx.x & 63, row = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + 16 * blockIdx.y;
-    const int64_t total = all_steps<ROWS, STEP>(a, lane);
-    const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
-    const int64_t u0 = (int64_t)blockIdx.x * share, u1 = u0 + share;
-    if (u1 >= total) return;                          // nothing goes on past the last share
-    const Place pl = place_of<ROWS, STEP>(a, u1 - 1, lane);
-    const int64_t local = u1 - 1 - pl.first;
-    const int item = (int)(local / pl.steps);
-    const int64_t begin = pl.first + (int64_t)item * pl.steps, end = begin + pl.steps;
-    if (begin < u0 || end <= u1) return;              // not begun here, or done here
-    const int rt = item / a.kv_heads, h = item - rt * a.kv_heads;
-    const int rows = (int)min((int64_t)ROWS, (int64_t)pl.s.n * a.group - (int64_t)rt * ROWS);
-    if (row >= rows) return;
-    const int parts = (int)((end - 1) / share - (int64_t)blockIdx.x) + 1;
-    // part 0 is this workgroup's second, the others are the first of theirs
-    auto part = [&](int i) { return a.part + (((int64_t)blockIdx.x + i) * 2 + (i == 0)) * kPartFloats<DH, ROWS>; };
-    float top = minus_inf();
-    for (int i = lane; i < parts; i += 64) top = fmaxf(top, part(i)[ROWS * DH + row]);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-    const float zero = top == minus_inf() ? 0.f : top;
-    float sum = 0.f, acc[N] = {};
-    for (int i = 0; i < parts; ++i) {
-        const float* p = part(i);
-        const float f = exp2_(p[ROWS * DH + row] - zero);
-        sum = fmaf(p[ROWS * DH + ROWS + row], f, sum);
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] = fmaf(p[row * DH + lane * N + e], f, acc[e]);
-    }
-    const uint32_t r = (uint32_t)rt * ROWS + row;
-    const int t = (int)divide(r, a.by_group), head = h * a.group + (int)(r - (uint32_t)t * a.group);
-    // a lane's N elements as two or more: a neighbour's is fetched where N is 1
-    if constexpr (N == 1) {
-        const float next = __shfl_down(acc[0], 1);
-        const float two[2] = {acc[0], next};
-        if ((lane & 1) == 0) finish_row<2>(a, pl.s.q0 + t, head, lane, two, sum, top);
-    } else {
-        finish_row<N>(a, pl.s.q0 + t, head, lane * N, acc, sum, top);
     }
 }
 
@@ -602,22 +675,22 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
     constexpr int LR = T / PIECES, NI = kManyTile / LR;     // rows of one round of loads, rounds of a tile
     constexpr int WR = 64 / PIECES;                         // rows that a wavefront loads
     __shared__ __align__(16) unsigned char smem[4 * BYTES]; // stage 0: K, V; stage 1: K, V
+    __shared__ int flag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
     const int lrow = threadIdx.x / PIECES, lpos = threadIdx.x % PIECES;
 
-    const int64_t total = all_steps<ROWS, STEP>(a, lane);
+    const Shares all = shares_of<ROWS, STEP>(a, lane);
     int64_t u, u_end;
     if constexpr (STEP == 0) {
         // one item a workgroup, the last ones (which see most) first
-        u = total - 1 - (int64_t)blockIdx.x;
+        u = all.total - 1 - (int64_t)blockIdx.x;
         if (u < 0) return;
         u_end = u + 1;
     } else {
-        const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
-        u = (int64_t)blockIdx.x * share;
-        u_end = min(u + share, total);
+        u = (int64_t)blockIdx.x * all.share;
+        u_end = min(u + all.share, all.total);
     }
     if constexpr (!FULL) {
         for (int i = threadIdx.x; i < 4 * BYTES / 16; i += T) reinterpret_cast<u32x4*>(smem)[i] = u32x4{};   // pieces past the head stay zero
@@ -845,29 +918,79 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
 
         // ---- results: a lane holds 4 elements after another of its row -------------------
         l += __shfl_xor(l, 32);
-        if (live) {
-            const float top = m == minus_inf() ? m : m * a.scale;
-            if (whole) {
+        float top = m == minus_inf() ? m : m * a.scale;
+        bool finish = whole;
+        if (STEP != 0 && !whole) {
+            // a part in the order of this kernel's registers, two floats of a lane at a
+            // time beside those of its neighbours
+            constexpr int F = kPartFloats<DH, ROWS>;
+            const int64_t begin = pl.first + (int64_t)item * pl.steps;
+            const Parts parts = parts_of(begin, begin + pl.steps, all.share);
+            const int at = wave * kManyRows * DH + 2 * lane;
+            finish = others_done(a, parts, &flag);
+            if (!finish) {
+                float* part = part_at<F>(a, parts, parts.mine);
+                if (works) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+                    for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const float acc[4] = {o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]};
-                        finish_row<4>(a, s.q0 + tok, head, 32 * d + 8 * v + 4 * half, acc, l, top);
-                    }
-            } else {
-                float* part = a.part + ((int64_t)blockIdx.x * 2 + (step0 == 0)) * kPartFloats<DH, ROWS>;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        *reinterpret_cast<f32x4*>(part + my * DH + 32 * d + 8 * v + 4 * half) =
-                            f32x4{o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]};
-                if (half == 0) {
-                    part[ROWS * DH + my] = top;
-                    part[ROWS * DH + ROWS + my] = l;
+                        for (int v = 0; v < 16; v += 2) put2(part + at + (d * 8 + v / 2) * 128, o[d][v], o[d][v + 1]);
+                    if (half == 0) put2(part + ROWS * DH + 2 * my, top, l);
                 }
+                finish = last_to_arrive(a, parts, &flag);
             }
+            if (finish) {
+                if (works) {
+                    // all parts in their order, this workgroup's from its registers
+                    float most = top;
+                    for (int i = 0; i < parts.count; ++i)
+                        if (i != parts.mine) most = fmaxf(most, get2(part_at<F>(a, parts, i) + ROWS * DH + 2 * my).x);
+                    const float z = most == minus_inf() ? 0.f : most;
+                    float l_all = 0.f;
+                    f32x16 o_all[DT];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) o_all[d][v] = 0.f;
+                    for (int i = 0; i < parts.count; ++i) {
+                        const float* part = part_at<F>(a, parts, i);
+                        if (i == parts.mine) {
+                            const float f = exp2_(top - z);
+                            l_all = fmaf(l, f, l_all);
+#pragma unroll
+                            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) o_all[d][v] = fmaf(o[d][v], f, o_all[d][v]);
+                        } else {
+                            const float2 ml = get2(part + ROWS * DH + 2 * my);
+                            const float f = exp2_(ml.x - z);
+                            l_all = fmaf(ml.y, f, l_all);
+#pragma unroll
+                            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                for (int v = 0; v < 16; v += 2) {
+                                    const float2 x = get2(part + at + (d * 8 + v / 2) * 128);
+                                    o_all[d][v] = fmaf(x.x, f, o_all[d][v]);
+                                    o_all[d][v + 1] = fmaf(x.y, f, o_all[d][v + 1]);
+                                }
+                        }
+                    }
+                    top = most;
+                    l = l_all;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d] = o_all[d];
+                }
+                joined(a, parts);
+            }
+        }
+        if (finish && live) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float acc[4] = {o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]};
+                    finish_row<4>(a, s.q0 + tok, head, 32 * d + 8 * v + 4 * half, acc, l, top);
+                }
         }
         __syncthreads();      // the tiles in shared memory are free
         u += step1 - step0;
@@ -899,11 +1022,8 @@ hipError_t few(const AttendArgs& a, hipStream_t s)
         hipLaunchKernelGGL(kernel, grid, dim3(kFewThreads), 0, s, a);
         return hipGetLastError();
     };
-    hipError_t e = a.dim == DH ? (pg16 ? launch(attend_few_kernel<DH, true, true>) : launch(attend_few_kernel<DH, false, true>))
-                               : (pg16 ? launch(attend_few_kernel<DH, true, false>) : launch(attend_few_kernel<DH, false, false>));
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((join_kernel<DH, kRows, kStep>), grid, dim3(1024), 0, s, a);
-    return hipGetLastError();
+    if (a.dim == DH) return pg16 ? launch(attend_few_kernel<DH, true, true>) : launch(attend_few_kernel<DH, false, true>);
+    return pg16 ? launch(attend_few_kernel<DH, true, false>) : launch(attend_few_kernel<DH, false, false>);
 }
 
 // Wavefronts of a workgroup of the kernel for many rows, and its workgroups of a
@@ -927,14 +1047,9 @@ hipError_t many(const AttendArgs& a, hipStream_t s)
         if (a.dim == DH) return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, true>, items) : launch(attend_many_kernel<DH, NW, 0, false, true>, items);
         return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, false>, items) : launch(attend_many_kernel<DH, NW, 0, false, false>, items);
     }
-    hipError_t e;
     if (a.dim == DH)
-        e = pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, true>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, true>, a.cus);
-    else
-        e = pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, false>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, false>, a.cus);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((join_kernel<DH, ROWS, kManyStep>), dim3((unsigned)a.cus, ROWS / 16), dim3(1024), 0, s, a);
-    return hipGetLastError();
+        return pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, true>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, true>, a.cus);
+    return pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, false>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, false>, a.cus);
 }
 
 template <int DH>
@@ -957,6 +1072,8 @@ hipError_t attend(const AttendArgs& args, hipStream_t s)
 
 }  // namespace
 
+size_t attend_groups(int cus) { return (size_t)std::max({kFewPerCu<64>, kFewPerCu<128>, kFewPerCu<256>, 1}) * cus; }
+
 size_t attend_part_floats(int dim, int cus)
 {
     return (size_t)cus * (dim <= 64 ? kGroupFloats<64> : dim <= 128 ? kGroupFloats<128> : kGroupFloats<256>);
@@ -969,7 +1086,6 @@ hipError_t launch_attend(const AttendArgs& args, hipStream_t s)
     a.by_group = divisor((uint32_t)a.group);
     a.by_page = divisor((uint32_t)a.cache.page_size);
     a.most = (int32_t)std::min((int64_t)a.step.table_width * a.cache.page_size, (int64_t)INT32_MAX - 4096);
-    a.least = 1;
     return a.dim <= 64 ? attend<64>(a, s) : a.dim <= 128 ? attend<128>(a, s) : attend<256>(a, s);
 }
 

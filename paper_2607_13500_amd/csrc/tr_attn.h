@@ -74,8 +74,8 @@ struct AttendArgs {
     int32_t group;             // heads / kv_heads
     Divisor by_group, by_page;
     int32_t most;              // tokens that a row of the table has pages for
-    int32_t least;             // steps of a workgroup's share, at least
     float* part;               // attend_part_floats of scratch
+    int32_t* arrived;          // attend_groups counts, zero between calls
     tr_heads q, out;
     tr_cache cache;
     tr_step step;
@@ -87,8 +87,9 @@ struct AttendArgs {
     int32_t cus;
 };
 
-// group, the divisors, most, least, scale, keep and flip are filled in by the launch.
+// group, the divisors, most, scale, keep and flip are filled in by the launch.
 size_t attend_part_floats(int dim, int cus);
+size_t attend_groups(int cus);
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
 
 // ---- device helpers ------------------------------------------------------------

@@ -30,6 +30,7 @@ struct tr_attn {
     int32_t* pair_axis = nullptr;   // [rot_dim / 2]
     float* part = nullptr;          // partial sums of dw
     float* parts = nullptr;         // parts of rows that several workgroups attend for (bf16)
+    int32_t* arrived = nullptr;     // and how many of an item's are there
 };
 
 namespace {
@@ -210,15 +211,17 @@ tr_status tr_attn_create(const tr_attn_params* p, tr_attn** out)
         return fail(TR_ENOMEM, "hipMalloc of a layer's tables failed: %s", hipGetErrorString(e));
     }
     if (p->dtype == TR_BF16 && p->head_dim % 8 == 0 &&
-        (e = al(&a->parts, tr::attend_part_floats(p->head_dim, a->cus) * sizeof(float))) != hipSuccess) {
+        ((e = al(&a->parts, tr::attend_part_floats(p->head_dim, a->cus) * sizeof(float))) != hipSuccess ||
+         (e = al(&a->arrived, tr::attend_groups(a->cus) * sizeof(int32_t))) != hipSuccess)) {
         tr_attn_destroy(a);
         return fail(TR_ENOMEM, "hipMalloc of a layer's scratch failed: %s", hipGetErrorString(e));
     }
     if ((e = hipMemcpy(a->freq, freq, sizeof freq, hipMemcpyHostToDevice)) != hipSuccess ||
         (e = hipMemcpy(a->pair_axis, axis, sizeof axis, hipMemcpyHostToDevice)) != hipSuccess ||
+        (a->arrived && (e = hipMemset(a->arrived, 0, tr::attend_groups(a->cus) * sizeof(int32_t))) != hipSuccess) ||
         (e = hipDeviceSynchronize()) != hipSuccess) {
         tr_attn_destroy(a);
-        return hip_fail(e, "table copy");
+        return hip_fail(e, "scratch initialisation");
     }
     log_line("attention context on device %d: %d query and %d key heads of %d, %d rotated over %d axes, %s%s", dev,
              p->heads, p->kv_heads, p->head_dim, p->rot_dim, p->axes, p->dtype == TR_BF16 ? "bf16" : "fp32",
@@ -235,6 +238,7 @@ void tr_attn_destroy(tr_attn* a)
     if (a->pair_axis) (void)hipFree(a->pair_axis);
     if (a->part) (void)hipFree(a->part);
     if (a->parts) (void)hipFree(a->parts);
+    if (a->arrived) (void)hipFree(a->arrived);
     delete a;
 }
 
@@ -432,6 +436,7 @@ tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const 
     r.window = window;
     r.lse = lse;
     r.part = a->parts;
+    r.arrived = a->arrived;
     r.cus = a->cus;
     hipError_t e = tr::launch_attend(r, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
