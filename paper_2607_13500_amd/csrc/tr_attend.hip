@@ -294,13 +294,23 @@ __device__ __forceinline__ void joined(const AttendArgs& a, const Parts& p)
     if (threadIdx.x == 0) __hip_atomic_store(a.arrived + p.owner, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Address swizzle of a row of V in shared memory, in pieces of 16 bytes: the 16
-// rows that a transposing read touches spread over all banks.
+// Address swizzles of a row in shared memory, in pieces of 16 bytes: the 16 rows
+// that a read of K's fragments, or a transposing read of V, touches spread over
+// all banks.
+template <int DH>
+__device__ __forceinline__ int k_swizzle(int row)
+{
+    return DH == 64 ? (row >> 1) & 7 : row & 15;
+}
+
 template <int DH>
 __device__ __forceinline__ int v_piece(int row, int piece)
 {
     return piece ^ ((DH == 64 ? (row >> 1) & 3 : row & 7) << 1);
 }
+
+// 16 bytes of keys or values that nothing reads again soon.
+__device__ __forceinline__ u32x4 read_once(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4*>(p)); }
 
 // Workgroups of a CU, by their registers.
 template <int DH>
@@ -315,7 +325,8 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
     constexpr int KF = DH / 32, DT = DH / 16;          // fragments of keys, tiles of elements
     constexpr int PIECES = DH / 8, VR = 64 / PIECES, VN = kTile / VR;   // pieces of a row, rows of a load, loads of a tile
     constexpr int PAD = DH + 4;
-    constexpr int kLds = 4 * (kTile * DH * 2 > kRows * PAD * 4 ? kTile * DH * 2 : kRows * PAD * 4);
+    constexpr int BYTES = kTile * DH * 2;
+    constexpr int kLds = 4 * (2 * BYTES > kRows * PAD * 4 ? 2 * BYTES : kRows * PAD * 4);
     __shared__ __align__(16) unsigned char smem[kLds];
     __shared__ float ml[4][2][kRows];
     __shared__ int flag;
@@ -323,9 +334,10 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
     const int vrow = lane / PIECES, piece = lane % PIECES;
-    unsigned char* vt = smem + wave * (kTile * DH * 2);
+    unsigned char* kt = smem + wave * 2 * BYTES;                 // the wavefront's tile
+    unsigned char* vt = kt + BYTES;
     const int token_bytes = (int)(a.cache.token * 2);            // PG16
-    const int k_lane = col * token_bytes + grp * 16, v_lane = vrow * token_bytes + piece * 16;
+    const int in_lane = vrow * token_bytes + piece * 16;
 
     const Shares all = shares_of<kRows, kStep>(a, lane);
     int64_t u = (int64_t)blockIdx.x * all.share;
@@ -380,7 +392,7 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
         const int last = hi_max - 1;              // tokens past it (and before lo_min) are read as it (as lo_min)
 
         auto page_at = [&](int slot) { return min(max(table[slot], 0), a.cache.pages - 1); };
-        u32x4 kr[2][KF], vr[VN];
+        u32x4 kr[VN], vr[VN];
         auto fetch = [&](int j) {
             if constexpr (PG16) {
 #pragma unroll
@@ -391,15 +403,14 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
                     const int slot = (int)divide((uint32_t)half, a.by_page);
                     const int64_t at = (int64_t)page_at(slot) * a.cache.page + (int64_t)(half - slot * a.cache.page_size) * a.cache.token;
                     const int64_t off = uniform(at);
-                    const char* kb = reinterpret_cast<const char*>(kp + off);
-                    const char* vb = reinterpret_cast<const char*>(vp + off);
-#pragma unroll
-                    for (int k = 0; k < KF; ++k)
-                        if (FULL || k * 32 + grp * 8 < a.dim) kr[x][k] = *reinterpret_cast<const u32x4*>(kb + k_lane + k * 64);
+                    const char* kb = reinterpret_cast<const char*>(kp + off) + in_lane;
+                    const char* vb = reinterpret_cast<const char*>(vp + off) + in_lane;
 #pragma unroll
                     for (int i = 0; i < VN / 2; ++i)
-                        if (FULL || piece * 8 < a.dim)
-                            vr[x * (VN / 2) + i] = *reinterpret_cast<const u32x4*>(vb + i * VR * token_bytes + v_lane);
+                        if (FULL || piece * 8 < a.dim) {
+                            kr[x * (VN / 2) + i] = read_once(kb + i * VR * token_bytes);
+                            vr[x * (VN / 2) + i] = read_once(vb + i * VR * token_bytes);
+                        }
                 }
             } else {
                 int64_t koff[2];
@@ -408,33 +419,23 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
                     const int t = min(max(j + 16 * x + col, lo_min), last);
                     const int slot = (int)divide((uint32_t)t, a.by_page);
                     koff[x] = (int64_t)page_at(slot) * a.cache.page + (int64_t)(t - slot * a.cache.page_size) * a.cache.token;
-#pragma unroll
-                    for (int k = 0; k < KF; ++k)
-                        if (FULL || k * 32 + grp * 8 < a.dim) kr[x][k] = *reinterpret_cast<const u32x4*>(kp + koff[x] + k * 32 + grp * 8);
                 }
 #pragma unroll
                 for (int i = 0; i < VN; ++i) {
                     const int64_t off = __shfl(koff[VR * i / 16], (VR * i + vrow) & 15) + piece * 8;
-                    if (FULL || piece * 8 < a.dim) vr[i] = *reinterpret_cast<const u32x4*>(vp + off);
+                    if (FULL || piece * 8 < a.dim) {
+                        kr[i] = read_once(kp + off);
+                        vr[i] = read_once(vp + off);
+                    }
                 }
             }
         };
         if constexpr (!FULL) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int k = 0; k < KF; ++k) kr[x][k] = u32x4{};   // pieces past the head stay zero
+            for (int i = 0; i < VN; ++i) kr[i] = u32x4{};   // pieces past the head stay zero
         }
         if (j0 < j_end) fetch(j0);
         for (; j0 < j_end; j0 += kStep) {
-            f32x4 sc[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < KF; ++k)
-                    sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[x][k]), qf[k], sc[x], 0, 0, 0);
-            }
             // rows that see different tokens of this tile: a value that is not
             // finite must not reach the rows that do not see it
             const bool mixed = lo_max > max(j0, lo_min) || hi_min < min(j0 + kTile, hi_max);
@@ -455,8 +456,23 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
             }
 #pragma unroll
             for (int i = 0; i < VN; ++i)
-                *reinterpret_cast<u32x4*>(vt + (VR * i + vrow) * (DH * 2) + v_piece<DH>(VR * i + vrow, piece) * 16) = vr[i];
+            {
+                const int row = VR * i + vrow;
+                *reinterpret_cast<u32x4*>(kt + row * (DH * 2) + (piece ^ k_swizzle<DH>(row)) * 16) = kr[i];
+                *reinterpret_cast<u32x4*>(vt + row * (DH * 2) + v_piece<DH>(row, piece) * 16) = vr[i];
+            }
             if (j0 + kStep < j_end) fetch(j0 + kStep);
+            f32x4 sc[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const int row = 16 * x + col;
+#pragma unroll
+                for (int k = 0; k < KF; ++k) {
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + row * (DH * 2) + ((4 * k + grp) ^ k_swizzle<DH>(row)) * 16);
+                    sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[k], sc[x], 0, 0, 0);
+                }
+            }
 
             // ---- weights ------------------------------------------------------------
             float p[8];
@@ -473,6 +489,7 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float m1 = fmaxf(m, top), zero = m1 == minus_inf() ? 0.f : m1;
+            const bool same = m1 == m;                // rows that see nothing yet among them
             const float keep = exp2_(m - zero);
             m = m1;
             l *= keep;
@@ -484,7 +501,7 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
             }
 #pragma unroll
             for (int v = 0; v < 4; ++v) pb[v] = pack_bf16(p[2 * v], p[2 * v + 1]);
-            if (!__all(keep == 1.f)) {
+            if (!__all(same)) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= keep;
             }
@@ -630,12 +647,6 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
 constexpr int kManyTile = 64, kManyRows = 32;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-template <int DH>
-__device__ __forceinline__ int k_swizzle(int row)
-{
-    return DH == 64 ? (row >> 1) & 7 : row & 15;
-}
 
 template <int DH>
 __device__ __forceinline__ int v_swizzle(int row)
