@@ -654,6 +654,42 @@ __device__ __forceinline__ int v_swizzle(int row)
     return DH == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
 }
 
+// Whether the workgroups take whole items in turn instead of equal shares of all
+// steps.  Shares count an item's steps as those of all its sequence's rows; where
+// tiles see only part of them (a prompt's, half of them on average; those under a
+// window, little more than it) the shares of such tiles are done sooner.  Taken
+// whole, the steps of the tiles themselves count, and half of the longest tile's
+// at the end while other workgroups have none left.
+template <int ROWS, int STEP>
+__device__ __forceinline__ bool items_alone(const AttendArgs& a, const Shares& all, int lane)
+{
+    if constexpr (STEP == 0) return true;
+    else {
+        if (!a.causal) return false;
+        float sum = 0.f, most = 0.f;
+        const float tile = (float)(ROWS / a.group + 1);             // new tokens of a tile
+        for (int b = lane; b < a.step.seqs; b += 64) {
+            const Sequence s = sequence_at(a, b);
+            if (s.n == 0) continue;
+            float mean = max(1.f, ((float)(s.end - s.begin) - 0.5f * max(0.f, (float)s.n - tile)) / STEP), top = (float)steps_of<STEP>(s);
+            if (a.window > 0) {
+                const float one = ((float)a.window + tile) / STEP + 1.f;
+                mean = min(mean, one);
+                top = min(top, one);
+            }
+            sum += mean * (float)tiles_of<ROWS>(a, s) * (float)a.kv_heads;
+            most = max(most, top);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            sum += __shfl_xor(sum, m);
+            most = max(most, __shfl_xor(most, m));
+        }
+        const float alone = max(most, sum / (float)gridDim.x + 0.5f * most);
+        return __all(alone < (float)all.share) != 0;
+    }
+}
+
 // 16 bytes a lane from memory into shared memory at lds + 16 lane.  An
 // instruction without a register result: the kernel counts and waits itself.
 __device__ __forceinline__ void load_lds(uint32_t lds, const void* p)
@@ -693,12 +729,12 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
     const int lrow = threadIdx.x / PIECES, lpos = threadIdx.x % PIECES;
 
     const Shares all = shares_of<ROWS, STEP>(a, lane);
-    int64_t u, u_end;
-    if constexpr (STEP == 0) {
-        // one item a workgroup, the last ones (which see most) first
-        u = all.total - 1 - (int64_t)blockIdx.x;
+    const bool by_item = STEP == 0 || items_alone<ROWS, STEP>(a, all, lane);
+    int64_t u, u_end = 0;
+    if (by_item) {
+        // whole items, the last ones (which see most) first
+        u = (STEP == 0 ? all.total : shares_of<ROWS, 0>(a, lane).total) - 1 - (int64_t)blockIdx.x;
         if (u < 0) return;
-        u_end = u + 1;
     } else {
         u = (int64_t)blockIdx.x * all.share;
         u_end = min(u + all.share, all.total);
@@ -707,14 +743,14 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
         for (int i = threadIdx.x; i < 4 * BYTES / 16; i += T) reinterpret_cast<u32x4*>(smem)[i] = u32x4{};   // pieces past the head stay zero
         __syncthreads();
     }
-    while (u < u_end) {
-        const Place pl = place_of<ROWS, STEP>(a, u, lane);
+    while (by_item ? u >= 0 : u < u_end) {
+        const Place pl = by_item ? place_of<ROWS, 0>(a, u, lane) : place_of<ROWS, STEP>(a, u, lane);
         const Sequence s = pl.s;
         const int64_t local = u - pl.first;
         const int item = (int)(local / pl.steps), step0 = (int)(local - (int64_t)item * pl.steps);
-        const int step1 = (int)min((int64_t)pl.steps, step0 + (u_end - u));
+        const int step1 = by_item ? 1 : (int)min((int64_t)pl.steps, step0 + (u_end - u));
         const int rt = item / a.kv_heads, h = item - rt * a.kv_heads;
-        const bool whole = step0 == 0 && step1 == pl.steps;
+        const bool whole = by_item || (step0 == 0 && step1 == pl.steps);
 
         // ---- rows: this lane's, the wavefront's and the workgroup's -------------------
         const int rows = (int)min((int64_t)ROWS, (int64_t)s.n * a.group - (int64_t)rt * ROWS);
@@ -754,7 +790,7 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
         const int base = s.begin & ~(kAlign - 1);
         int j0 = base + step0 * STEP;
         if (lo_min > j0) j0 += (lo_min - j0) / kManyTile * kManyTile;   // tiles that no row sees are skipped
-        const int j_end = STEP == 0 ? hi_max : min(hi_max, base + step1 * STEP);
+        const int j_end = by_item ? hi_max : min(hi_max, base + step1 * STEP);
         const int last = hi_max - 1;
         const int32_t* table = a.step.table + (int64_t)pl.b * a.step.table_stride;
         const uint16_t* kp = static_cast<const uint16_t*>(a.cache.k) + (int64_t)h * a.cache.head;
@@ -1003,8 +1039,9 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
                     finish_row<4>(a, s.q0 + tok, head, 32 * d + 8 * v + 4 * half, acc, l, top);
                 }
         }
+        if constexpr (STEP == 0) return;
         __syncthreads();      // the tiles in shared memory are free
-        u += step1 - step0;
+        u += by_item ? -(int64_t)gridDim.x : (int64_t)(step1 - step0);
     }
 }
 
