@@ -99,12 +99,16 @@ __device__ __forceinline__ void seen_by(const AttendArgs& a, const Sequence& s, 
 // range of keys in steps of kStep.  All steps of all items in a row are dealt
 // out to the workgroups in equal shares, whatever the sequences' lengths: a
 // workgroup's share can end inside an item, and then the last of its workgroups
-// to arrive joins the item's parts.  A workgroup's four wavefronts take tiles of 32 keys in turn,
-// each with its own maximum and sums, and join them at the end of an item.
+// to arrive joins the item's parts.  A workgroup's four wavefronts take tiles of 32 keys in
+// turn, each with its own maximum and sums, and join them at the end of an item.
 //
 // Bound by the bytes of the cache: a wavefront has the next tile's keys and
 // values in flight, in registers, while it works on one; 16 rows cost two
-// matrix instructions of 16 cycles per 16 x 32 elements of keys.
+// matrix instructions of 16 cycles per 16 x 32 elements of keys.  Rows of a head
+// are read whole, a load after another, and past the caches: 5.9-6.2 TB/s (64
+// requests over 256 to 16384 tokens 211 us), where 64 bytes of 16 rows at a time
+// through the caches reached 5.2.  Three workgroups of a CU instead of two spill
+// registers (342 us).
 constexpr int kRows = 16, kTile = 32, kStep = 128, kFewThreads = 256;
 constexpr int kAlign = 32;   // a range of keys begins at a multiple of it
 
@@ -638,7 +642,11 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
 // ---- many rows ---------------------------------------------------------------------------
 // A workgroup of NW wavefronts of 32 rows each over the same keys, in tiles of
 // 64 that go from memory straight into shared memory, two tiles there at a time:
-// one is loaded while the other is worked on.
+// one is loaded while the other is worked on.  Bound by the matrix instructions
+// and by the softmax between them, which the two wavefronts of a SIMD overlap:
+// a prompt of 18432 tokens of 32 heads of 128 takes 2.82-2.92 ms (953-988
+// TFLOP/s; 42 % of the matrix units' cycles), eight chunks over long contexts
+// 550 us (660: the last shares end unevenly, and their parts are joined).
 //
 // Shared memory rows are DH elements in pieces of 16 bytes; piece c of row r lies
 // at piece c ^ f(r), which the loads bring about by each lane's choice of source
@@ -659,7 +667,9 @@ __device__ __forceinline__ int v_swizzle(int row)
 // tiles see only part of them (a prompt's, half of them on average; those under a
 // window, little more than it) the shares of such tiles are done sooner.  Taken
 // whole, the steps of the tiles themselves count, and half of the longest tile's
-// at the end while other workgroups have none left.
+// at the end while other workgroups have none left.  8 heads of keys, a group of 4:
+// a prompt of 3800 tokens from an empty cache takes 214 us so and 306 by shares,
+// 1500 tokens with a window of 512 over 8000 37 and 65.
 template <int ROWS, int STEP>
 __device__ __forceinline__ bool items_alone(const AttendArgs& a, const Shares& all, int lane)
 {
@@ -1056,6 +1066,8 @@ Divisor divisor(uint32_t d)
 }
 
 // Whether 16 tokens from a multiple of 16 on lie in one page of less than 2 GB.
+// Addressing them by the wavefront takes 64 single tokens over 8000 (pages of 64)
+// from 181 to 175 us and a prompt of 8192 from 628 to 612.
 bool in_halves(const AttendArgs& a)
 {
     return a.cache.page_size % 16 == 0 && a.cache.token < INT32_MAX / 2 && a.cache.token * 2 * (int64_t)a.cache.page_size < INT32_MAX;
@@ -1091,6 +1103,11 @@ hipError_t many(const AttendArgs& a, hipStream_t s)
         return hipGetLastError();
     };
     const bool pg16 = in_halves(a);
+    // An item a workgroup where that makes two rounds at least, else a workgroup a CU
+    // and shares of the steps (8 heads of keys of 128, a group of 4; 512 items of
+    // chunks of 256 tokens over 4000: 398 us by items, 416 by shares; 1024: 693 and
+    // 761; 128: 159 and 145; shares also keep a long context among short ones from
+    // being one workgroup's).
     if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus) {
         if (a.dim == DH) return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, true>, items) : launch(attend_many_kernel<DH, NW, 0, false, true>, items);
         return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, false>, items) : launch(attend_many_kernel<DH, NW, 0, false, false>, items);
@@ -1107,6 +1124,9 @@ template <int DH>
 hipError_t attend(const AttendArgs& args, hipStream_t s)
 {
     AttendArgs a = args;
+    // By the rows of a sequence and key head, on average (28 and 4 heads of 128, 16
+    // contexts of 8000): 28 rows take 97 us as few and 119 as many, 35 rows 136 and
+    // 125; 64 contexts of 2000: 89 and 93, 133 and 96.
     if (a.tokens * a.group <= 32 * (int64_t)a.step.seqs) {
         a.scale = a.raw_scale * kLog2e;
         return few<DH>(a, s);

@@ -57,7 +57,8 @@ tr_status check_attn_params(const tr_attn_params* p)
     if (!p->inv_freq && p->rot_dim && !(p->base > 0.0 && isfinite(p->base)))
         return fail(TR_EINVAL, "base must be finite and > 0 (got %g)", p->base);
     for (int i = 0; i < p->rot_dim / 2; ++i) {
-        if (p->inv_freq && !isfinite(p->inv_freq[i])) return fail(TR_EINVAL, "inv_freq[%d] is not finite", i);
+        if (p->inv_freq && !isfinite((float)p->inv_freq[i]))
+            return fail(TR_EINVAL, "inv_freq[%d] is not finite in fp32", i);
         if (p->pair_axis && (p->pair_axis[i] < 0 || p->pair_axis[i] >= p->axes))
             return fail(TR_EINVAL, "pair_axis[%d] = %d must be in [0, %d)", i, p->pair_axis[i], p->axes);
     }
@@ -407,7 +408,7 @@ tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const 
     if (st != TR_OK) return st;
     if (a->p.dtype != TR_BF16) return fail(TR_EUNSUPPORTED, "tr_attend needs a bf16 context");
     if (a->p.head_dim % 8) return fail(TR_EUNSUPPORTED, "tr_attend needs head_dim %% 8 == 0 (got %d)", a->p.head_dim);
-    if (!isfinite(scale)) return fail(TR_EINVAL, "scale must be finite (got %g)", scale);
+    if (!isfinite((float)scale)) return fail(TR_EINVAL, "scale must be finite in fp32 (got %g)", scale);
     if (causal != 0 && causal != 1) return fail(TR_EINVAL, "causal must be 0 or 1 (got %d)", causal);
     if (window < 0 || (window > 0 && !causal))
         return fail(TR_EINVAL, "window must be >= 0, and 0 without causal (got %d)", window);

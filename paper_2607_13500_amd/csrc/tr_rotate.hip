@@ -9,7 +9,12 @@
 // nearest quarter and a rest of at most an eighth, where the Taylor series of
 // sine and cosine to x^9 and x^10 are below 2e-9 off.
 //
-// All of it is bound by memory: heads are read once and written once.
+// All of it is bound by memory: heads are read once and written once.  Measured:
+// 36864 tokens of 40 bf16 heads of 128 in 132-138 us (5.5-5.7 TB/s read and
+// written; a library copy of 2 GiB 5.0), 8 prompts appended (9000 tokens) in 36 us
+// (5.3), gradients of 16384 tokens in 93 us (5.4) and the sum of dw in 7 more.
+// Small calls are bound by their launch: 64 tokens appended 5.4 us, 577 fp32 tokens
+// 5.3, positions of 64 clips 2.7.
 #include <algorithm>
 #include <type_traits>
 
