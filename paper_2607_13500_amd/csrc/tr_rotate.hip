@@ -12,7 +12,7 @@
 // All of it is bound by memory: heads are read once and written once.  Measured:
 // 36864 tokens of 40 bf16 heads of 128 in 132-138 us (5.5-5.7 TB/s read and
 // written; a library copy of 2 GiB 5.0), 8 prompts appended (9000 tokens) in 36 us
-// (5.3), gradients of 16384 tokens in 93 us (5.4) and the sum of dw in 7 more.
+// (5.3), gradients of 16384 tokens in 93 us (5.4) and the sum of dw in 5 more.
 // Small calls are bound by their launch: 64 tokens appended 5.4 us, 577 fp32 tokens
 // 5.3, positions of 64 clips 2.7.
 #include <algorithm>
@@ -292,9 +292,18 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(RotateArgs g, int parts
     const int kind = blockIdx.y, col = threadIdx.x & 31, row = threadIdx.x >> 5;
     const int j = blockIdx.x * 32 + col;
     if (!g.dw[kind]) return;   // the whole workgroup leaves together
+    constexpr int U = 8;                     // rows of a column on their way at a time
     float s = 0.f;
-    if (j < g.dim)
-        for (int i = row; i < parts; i += 32) s += g.part[((int64_t)kind * parts + i) * g.dim + j];
+    for (int i0 = row; i0 < parts; i0 += 32 * U) {
+        float v[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int i = i0 + 32 * k;
+            v[k] = i < parts && j < g.dim ? g.part[((int64_t)kind * parts + i) * g.dim + j] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) s += v[k];
+    }
     red[row][col] = s;
     __syncthreads();
     if (threadIdx.x < 32) {
