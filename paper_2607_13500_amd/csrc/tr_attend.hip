@@ -37,21 +37,22 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float from_bf16(uint32_t v) { return __uint_as_float(v << 16); }
 
-// The largest of three, numbers before NaN, in one instruction (fmaxf of a matrix
-// instruction's result first quiets it in another).
+// The largest of three, NaN if one is: one instruction, and one that does not
+// first quiet a matrix instruction's result in another, as fmaxf does.  Both of
+// these stay in the compiler's hands: between a matrix instruction or an
+// exponential and a reader of its result there have to be waits, which it counts
+// for its own instructions and not for those of inline assembly.
 __device__ __forceinline__ float max3(float x, float y, float z)
 {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
-    return r;
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z);
 }
 
 // Two values rounded to bf16, the first one low.
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
 {
-    uint32_t r;
-    asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
-    return r;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
 }
 
 // Whether a word holds a bf16 that is not finite.

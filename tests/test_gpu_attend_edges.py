@@ -1,0 +1,77 @@
+"""Attention's edges in each of its kernels: the one for few rows, and the one for
+many by shares of all steps, by whole items in turn, and by an item a workgroup.
+Tolerances as in test_gpu_attend."""
+import math
+
+import pytest
+import torch
+
+import paper_2607_13500_amd as tr
+from test_gpu_attend import normal_caches
+from test_gpu_rotate import BF, DEV, gen, on_device, say, step_of
+
+pytestmark = pytest.mark.gpu
+
+# new tokens, lengths, heads, key heads, causal
+KERNELS = {"few": ([3, 1], [700, 90], 4, 2, True), "shares": ([70, 130], [701, 300], 4, 2, False),
+           "in_turn": ([1200], [1200], 80, 80, True), "items": ([2048], [2050], 64, 64, True)}
+
+
+def definition(q, cache, step, scale, causal, window=0):
+    """(out, lse, sum w |v|, largest |score|) in 64 bits, a head of a sequence at a time."""
+    page, group = cache.k.shape[1], q.shape[1] // cache.k.shape[2]
+    out, mass = (torch.zeros(q.shape, dtype=torch.float64, device=DEV) for _ in range(2))
+    lse, most = (torch.zeros(q.shape[:2], dtype=torch.float64, device=DEV) for _ in range(2))
+    for b, kv in enumerate(step.kv_len.tolist()):
+        t0, t1 = step.q_start[b].item(), step.q_start[b + 1].item()
+        j = torch.arange(kv, device=DEV)
+        rows = step.table[b].to(DEV).long()[j // page] * page + j % page
+        behind = torch.arange(kv - (t1 - t0), kv, device=DEV)[:, None] - j
+        hide = (behind < 0) & causal
+        if window:
+            hide = hide | (behind >= window)
+        for h in range(q.shape[1]):
+            k, v = (c.flatten(0, 1)[rows, h // group].double() for c in cache)
+            s = torch.matmul(q[t0:t1, h].double(), k.t().contiguous()) * scale
+            most[t0:t1, h] = s.masked_fill(hide, 0.0).abs().amax(1)
+            s = s.masked_fill(hide, -math.inf)
+            lse[t0:t1, h] = torch.logsumexp(s, 1)
+            w = torch.exp(s - lse[t0:t1, h, None])
+            out[t0:t1, h], mass[t0:t1, h] = torch.matmul(w, v), torch.matmul(w, v.abs())
+    return out, lse, mass, most
+
+
+def compare(a, q, cache, step, scale, causal):
+    got, got_lse = a.attend(q, cache, on_device(step), scale=scale, causal=causal, want_lse=True)
+    again, _ = a.attend(q, cache, on_device(step), scale=scale, causal=causal)
+    assert torch.equal(got, again)
+    want, lse, mass, most = definition(q, cache, step, scale, causal)
+    assert torch.isfinite(got).all() and torch.isfinite(got_lse).all()
+    assert float(((got.double() - want).abs() - 2.0 ** -8 * want.abs() - (2.0 ** -8 + 1.5e-3) * mass).max()) <= 0.0
+    assert float(((got_lse.double() - lse).abs() - 2e-5 * (1.0 + most)).max()) <= 0.0
+
+
+def inputs(kernel, dim, page_size, g):
+    new, kv, heads, kv_heads, causal = KERNELS[kernel]
+    step, pages = step_of(new, kv, page_size, g)
+    return (torch.randn(sum(new), heads, dim, generator=g).to(BF), normal_caches(pages, page_size, kv_heads, dim, g), step,
+            tr.Attention(heads, kv_heads, dim, BF), causal)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 80, 256])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_partial_sums_that_cancel(kernel, dim):
+    """Scores of ordinary size whose sums over the first elements of a head are
+    thousands: the last elements take them back.  All elements are multiples of 1/8
+    of at most 16, so every partial sum (below 2^13, a multiple of 2^-6) is exact."""
+    say("cancel", kernel, dim)
+    g = gen(dim)
+    q, cache, step, a, causal = inputs(kernel, dim, 16, g)
+    eighths = lambda t: (8.0 * t.float()).round().clamp(-24, 24) / 8.0
+    for sign in (1.0, -1.0):          # the partial sums far above, and far below
+        q = eighths(q).to(BF)
+        q[..., :16] = q[..., dim - 16:] = 16.0
+        cache.k.copy_(eighths(cache.k))
+        cache.k[..., :16], cache.k[..., dim - 16:] = 16.0 * sign, -16.0 * sign
+        compare(a, q.to(DEV), cache, step, 1.0 / math.sqrt(dim), causal)
+    a.close()
