@@ -860,9 +860,11 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
             const unsigned char* kt = smem + stage * 2 * BYTES;
             unsigned char* vt = smem + stage * 2 * BYTES + BYTES;
 
-            // a value that is not finite must not reach rows that do not see it
+            // a value that is not finite must not reach rows that do not see it, nor, by
+            // the weight 0 of a key past the ends (which holds a seen one's value),
+            // elements that are infinite
             bool bad = false;
-            if (lo_max > max(j0, lo_min) || hi_min < min(j0 + kManyTile, hi_max)) {
+            if (j0 < lo_max || j0 + kManyTile > hi_min) {
                 bool mine = false;
                 for (int i = threadIdx.x; i < BYTES / 16; i += T) {
                     const u32x4 w = *reinterpret_cast<const u32x4*>(vt + i * 16);

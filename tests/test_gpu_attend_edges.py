@@ -75,3 +75,34 @@ def test_partial_sums_that_cancel(kernel, dim):
         cache.k[..., :16], cache.k[..., dim - 16:] = 16.0 * sign, -16.0 * sign
         compare(a, q.to(DEV), cache, step, 1.0 / math.sqrt(dim), causal)
     a.close()
+
+
+@pytest.mark.parametrize("new,kv,heads,kv_heads,causal,window", [
+    ([64], [50], 2, 2, False, 0), ([70, 90], [64, 129], 4, 2, False, 0), ([1], [90], 33, 1, True, 20), ([1, 1], [65, 700], 40, 1, True, 0),
+    ([2048], [70], 64, 64, False, 0), ([2], [50], 2, 2, False, 0)])
+def test_infinite_values_at_the_ends_of_what_is_seen(new, kv, heads, kv_heads, causal, window):
+    """All rows see the same keys, whose first and last values are infinite: those
+    elements are infinite, all others as they are without."""
+    for dim, page_size in ((64, 16), (128, 48), (80, 7), (256, 16)):
+        say("ends", new, kv, heads, causal, window, dim)
+        g = gen(dim + heads)
+        step, pages = step_of(new, kv, page_size, g)
+        cache = normal_caches(pages, page_size, kv_heads, dim, g)
+        q = torch.randn(sum(new), heads, dim, generator=g).to(BF).to(DEV)
+        a = tr.Attention(heads, kv_heads, dim, BF)
+        ends = []
+        for b, n in enumerate(kv):
+            for j in (max(0, n - window) if window else 0, n - 1):
+                ends.append((int(step.table[b, j // page_size]), j % page_size))
+        for e, (page, row) in zip((3, 40, 5, 6), ends):
+            cache.v[page, row, :, e] = 0.0
+        clean, lse = a.attend(q, cache, on_device(step), causal=causal, window=window, want_lse=True)
+        want = clean.clone()
+        for i, (e, (page, row)) in enumerate(zip((3, 40, 5, 6), ends)):
+            sign = -1.0 if i % 2 else 1.0
+            cache.v[page, row, :, e] = sign * math.inf
+            first = sum(new[:i // 2])
+            want[first:first + new[i // 2], :, e] = sign * math.inf
+        got, got_lse = a.attend(q, cache, on_device(step), causal=causal, window=window, want_lse=True)
+        assert torch.equal(got, want) and torch.equal(got_lse, lse)
+        a.close()
