@@ -106,3 +106,65 @@ def test_infinite_values_at_the_ends_of_what_is_seen(new, kv, heads, kv_heads, c
         got, got_lse = a.attend(q, cache, on_device(step), causal=causal, window=window, want_lse=True)
         assert torch.equal(got, want) and torch.equal(got_lse, lse)
         a.close()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_scores_of_every_size(kernel, dim):
+    """Scales of both signs and zero, a running maximum that rises all the way, one
+    key far above the others, scores all far below zero."""
+    say("scores", kernel, dim)
+    g = gen(dim + 1)
+    q, cache, step, a, causal = inputs(kernel, dim, 16, g)
+    q = q.to(DEV)
+    for scale in (0.0, -0.125, 1e-3, -1e-30):
+        compare(a, q, cache, step, scale, causal)
+    kept = cache.k.clone()
+    most = max(step.kv_len.tolist())
+    # of equal elements: sums over a head are exact.  Up, then down
+    fours = torch.full_like(q, 4.0)
+    rise = torch.arange(most, dtype=torch.float32) * 0.004
+    for b, kv in enumerate(step.kv_len.tolist()):
+        j = torch.arange(kv)
+        cache.k[step.table[b].long()[j // 16].to(DEV), (j % 16).to(DEV)] = rise[:kv].to(BF).to(DEV)[:, None, None]
+    for scale in (1.0 / math.sqrt(dim), -1.0 / math.sqrt(dim)):
+        compare(a, fours, cache, step, scale, causal)
+    cache.k.copy_(kept)
+    for b, kv in enumerate(step.kv_len.tolist()):
+        cache.k[int(step.table[b, (kv * 3 // 4) // 16]), (kv * 3 // 4) % 16] = 30.0
+    compare(a, fours, cache, step, 1.0 / math.sqrt(dim), causal)
+    cache.k.copy_(-kept.abs() - 20.0)
+    compare(a, (20.0 + 0.01 * q.float()).to(BF), cache, step, 0.125 / 400, causal)
+    a.close()
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_not_finite_values_that_are_seen(kernel):
+    """A NaN key makes the rows NaN that see it; a value's NaN or infinity stays in
+    its element, of the rows that see it."""
+    say("seen", kernel)
+    dim, at = 64, 41
+    new, kv, _, kv_heads, causal = KERNELS[kernel]
+    q, cache, step, a, causal = inputs(kernel, dim, 16, gen(3))
+    q, group = q.to(DEV), a.heads // kv_heads
+    clean, lse = a.attend(q, cache, on_device(step), causal=causal, want_lse=True)
+    page, row = int(step.table[0, at // 16]), at % 16
+    sees = torch.zeros(sum(new), dtype=torch.bool, device=DEV)
+    sees[:new[0]] = torch.arange(new[0], device=DEV) + kv[0] - new[0] >= at if causal else True
+    cache.v[page, row, 1, 5], cache.v[page, row, 0, 9], cache.v[page, row, 1, 63] = math.inf, math.nan, -math.inf
+    out, out_lse = a.attend(q, cache, on_device(step), causal=causal, want_lse=True)
+    assert torch.equal(out[~sees], clean[~sees]) and torch.equal(out_lse, lse)
+    first, second = slice(0, group), slice(group, 2 * group)
+    assert (out[sees, second, 5] == math.inf).all() and (out[sees, second, 63] == -math.inf).all() and torch.isnan(out[sees, first, 9]).all()
+    out[sees, second, 5] = out[sees, second, 63] = out[sees, first, 9] = 0.0
+    cache.v[page, row, 1, 5], cache.v[page, row, 0, 9], cache.v[page, row, 1, 63] = 0.0, 0.0, 0.0
+    want, _ = a.attend(q, cache, on_device(step), causal=causal)
+    want[sees, second, 5] = want[sees, second, 63] = want[sees, first, 9] = 0.0
+    assert torch.equal(out, want)
+    cache.k[page, row, 1, 7] = math.nan
+    out, out_lse = a.attend(q, cache, on_device(step), causal=causal, want_lse=True)
+    assert torch.isnan(out[sees][:, second]).all() and torch.isnan(out_lse[sees][:, second]).all()
+    others = torch.ones(a.heads, dtype=torch.bool, device=DEV)
+    others[second] = False
+    assert torch.equal(out_lse[:, others], lse[:, others]) and torch.equal(out_lse[~sees], lse[~sees])
+    a.close()
