@@ -787,7 +787,13 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
             u32x4 v{};
             if (live && (FULL || k * 16 + half * 8 < a.dim))
                 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q.p) + (s.q0 + tok) * a.q.token + (int64_t)head * a.q.head + k * 16 + half * 8);
-            v = (v & a.keep) ^ a.flip;            // scale < 0: that of -q; scale 0: scores of q = 0
+            // scale < 0: that of -q; scale 0: scores of q = 0, NaN where it is not finite
+            if (a.keep == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[i] = ((v[i] & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u);
+            }
+            v ^= a.flip;
             qf[k] = __builtin_bit_cast(bf16x8, v);
         }
         f32x16 o[DT];

@@ -81,7 +81,7 @@ struct AttendArgs {
     tr_step step;
     float raw_scale;           // of the scores
     float scale;               // the same in powers of two
-    uint32_t keep, flip;       // bits of q to keep and then to flip, where scale has to be > 0
+    uint32_t keep, flip;       // 0: scale is 0, q counts as 0; bits of q to flip, where scale has to be > 0
     int32_t causal, window;
     float* lse;                // [tokens, heads] or nullptr
     int32_t cus;

@@ -168,3 +168,19 @@ def test_not_finite_values_that_are_seen(kernel):
     others[second] = False
     assert torch.equal(out_lse[:, others], lse[:, others]) and torch.equal(out_lse[~sees], lse[~sees])
     a.close()
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_scale_zero_of_queries_that_are_not_finite(kernel):
+    """0 times a sum that is not finite is NaN, and so is its row; the others are means."""
+    say("scale 0", kernel)
+    q, cache, step, a, causal = inputs(kernel, 64, 16, gen(8))
+    q = q.to(DEV)
+    clean, lse = a.attend(q, cache, on_device(step), scale=0.0, causal=causal, want_lse=True)
+    q[1, 0, 7], q[2, 3, 8], q[2, 1, 63] = math.nan, math.inf, -math.inf
+    out, out_lse = a.attend(q, cache, on_device(step), scale=0.0, causal=causal, want_lse=True)
+    for t, h in ((1, 0), (2, 3), (2, 1)):
+        assert torch.isnan(out[t, h]).all() and torch.isnan(out_lse[t, h])
+        out[t, h], out_lse[t, h] = clean[t, h], lse[t, h]
+    assert torch.equal(out, clean) and torch.equal(out_lse, lse)
+    a.close()
