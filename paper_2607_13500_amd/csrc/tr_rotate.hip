@@ -206,11 +206,11 @@ struct AnyHead {
 };
 
 template <typename E>
-__global__ __launch_bounds__(256) void rotate_any_kernel(RotateArgs g)
+__global__ __launch_bounds__(256) void rotate_any_kernel(RotateArgs g, int64_t first)
 {
     const int lane = threadIdx.x & 63;
     const int rows = g.heads[0] + g.heads[1] + g.heads[2];
-    const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t u = first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (u >= g.tokens * rows) return;
     const int64_t t = u / rows;
     int h = (int)(u - t * rows), kind = 0;
@@ -470,15 +470,15 @@ __device__ __forceinline__ void put(E* p, Raw<E> v)
     else *reinterpret_cast<Raw<E>*>(p) = v;
 }
 
-// A wavefront takes `per` rounds of one token, a round being 64 / LP heads of
-// one side: queries, keys, then values.  A head's address is the round's (the
+// Wavefront `first` and those after it: each takes `per` rounds of one token, a
+// round being 64 / LP heads of one side: queries, keys, then values.  A head's address is the round's (the
 // wavefront's) and 32 bits of a lane's.
 template <typename E, int LP, bool ADJ, bool APPEND, bool STREAM>
-__global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int chunks)
+__global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int chunks, uint32_t first)
 {
     constexpr int R = 64 / LP, DEPTH = 2;
     const int lane = threadIdx.x & 63, j = lane & (LP - 1), hl = lane / LP;
-    const uint32_t u = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t u = first + blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t t = u / (uint32_t)chunks;
     if (t >= g.tokens) return;
     const int n0 = (g.heads[0] + R - 1) / R, n1 = n0 + (g.heads[1] + R - 1) / R, all = n1 + (g.heads[2] + R - 1) / R;
@@ -701,6 +701,20 @@ bool in_pieces(const RotateArgs& a, int eb, bool back)
                          (a.cache.page | a.cache.token | a.cache.head) % kPiece == 0);
 }
 
+// Launches f(first, workgroups) for n wavefronts, four to a workgroup: a launch
+// has fewer than 2^32 threads.
+template <typename F>
+hipError_t in_launches(int64_t n, F f)
+{
+    constexpr int64_t kMost = int64_t(1) << 25;
+    hipError_t e = hipSuccess;
+    for (int64_t first = 0; first < n && e == hipSuccess; first += kMost) {
+        f(first, (unsigned)((std::min(kMost, n - first) + 3) / 4));
+        e = hipGetLastError();
+    }
+    return e;
+}
+
 // From what a call moves on its stores are streamed.
 constexpr int64_t kStreamBytes = 32 << 20;
 
@@ -717,11 +731,11 @@ hipError_t rotate_pieces(const RotateArgs& a, hipStream_t s)
     // where that leaves the chip full; else a round each.
     const int per = a.tokens >= 16 * (int64_t)a.cus ? rounds : 1;
     const int chunks = (rounds + per - 1) / per;
-    const int64_t groups = (a.tokens * chunks + 3) / 4;
     const bool stream = a.tokens * heads * a.dim * (int64_t)sizeof(E) >= kStreamBytes;
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, s, a, per, chunks);
-        return hipGetLastError();
+        return in_launches(a.tokens * chunks, [&](int64_t first, unsigned groups) {
+            hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, s, a, per, chunks, (uint32_t)first);
+        });
     };
     auto pick = [&](auto adj, auto append) {
         constexpr bool A = decltype(adj)::value, P = decltype(append)::value;
@@ -749,9 +763,9 @@ template <typename E>
 hipError_t rotate_typed(const RotateArgs& a, hipStream_t s)
 {
     if (!in_pieces(a, (int)sizeof(E), false)) {
-        const int64_t rows = a.tokens * (a.heads[0] + a.heads[1] + a.heads[2]);
-        hipLaunchKernelGGL(rotate_any_kernel<E>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
-        return hipGetLastError();
+        return in_launches(a.tokens * (a.heads[0] + a.heads[1] + a.heads[2]), [&](int64_t first, unsigned groups) {
+            hipLaunchKernelGGL(rotate_any_kernel<E>, dim3(groups), dim3(256), 0, s, a, first);
+        });
     }
     const int lanes = a.dim / (2 * kPiece);
     if (lanes <= 4) return rotate_pieces<E, 4>(a, s);
