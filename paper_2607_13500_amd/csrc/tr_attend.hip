@@ -1116,8 +1116,8 @@ hipError_t many(const AttendArgs& a, hipStream_t s)
     // and shares of the steps (8 heads of keys of 128, a group of 4; 512 items of
     // chunks of 256 tokens over 4000: 398 us by items, 416 by shares; 1024: 693 and
     // 761; 128: 159 and 145; shares also keep a long context among short ones from
-    // being one workgroup's).
-    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus) {
+    // being one workgroup's).  A launch has fewer than 2^32 threads.
+    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus && items * (NW * 64) <= (int64_t)UINT32_MAX) {
         if (a.dim == DH) return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, true>, items) : launch(attend_many_kernel<DH, NW, 0, false, true>, items);
         return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, false>, items) : launch(attend_many_kernel<DH, NW, 0, false, false>, items);
     }

@@ -184,3 +184,23 @@ def test_scale_zero_of_queries_that_are_not_finite(kernel):
         out[t, h], out_lse[t, h] = clean[t, h], lse[t, h]
     assert torch.equal(out, clean) and torch.equal(out_lse, lse)
     a.close()
+
+
+def test_more_items_than_a_launch_has_threads_for():
+    """2^23 tiles of 256 rows and more, of 512 threads each.  Keys of zeros and equal
+    values, so that every row of a sequence is its value exactly."""
+    seqs, heads, dim, tokens, page_size = 1000, 65535, 8, 32766, 16
+    say("large", seqs, heads, tokens)
+    a = tr.Attention(heads, 1, dim, BF)
+    assert (tokens * heads + seqs * 256) * 2 >= 2 ** 32
+    value = (torch.arange(seqs, device=DEV) % 200 + 1).to(BF)
+    cache = tr.KVCache(torch.zeros(seqs, page_size, 1, dim, dtype=BF, device=DEV), value[:, None, None, None].expand(seqs, page_size, 1, dim).contiguous())
+    q_start = (torch.arange(seqs + 1, device=DEV) * tokens // seqs).to(torch.int32)
+    step = tr.Step(q_start, torch.full((seqs,), 11, dtype=torch.int32, device=DEV), torch.arange(seqs, dtype=torch.int32, device=DEV)[:, None])
+    q = torch.ones(1, 1, dim, dtype=BF, device=DEV).expand(tokens, heads, dim)
+    out = torch.zeros(tokens, heads, dim, dtype=BF, device=DEV)
+    a.attend(q, cache, step, causal=False, out=out)
+    want = torch.repeat_interleave(value, (q_start[1:] - q_start[:-1]).long())
+    for t in range(0, tokens, 4096):
+        assert (out[t:t + 4096] == want[t:t + 4096, None, None]).all()
+    a.close()
