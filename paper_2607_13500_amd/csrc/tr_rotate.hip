@@ -29,8 +29,8 @@ namespace {
 __global__ __launch_bounds__(256) void positions_kernel(PosArgs a)
 {
     const PosImage im = a.image[blockIdx.y];
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= im.count) return;
+    const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;   // the last workgroup's may pass 2^31
+    if (i >= (uint32_t)im.count) return;
     const int32_t n = a.idx[im.src + i];
     const int32_t t = n / im.hw, in = n - t * im.hw;
     const int32_t h = in / im.w, w = in - h * im.w;
@@ -801,7 +801,7 @@ hipError_t back_typed(const RotateArgs& a, hipStream_t s)
 hipError_t launch_positions(const PosArgs& a, int images, int most, hipStream_t s)
 {
     if (images < 1 || most < 1) return hipSuccess;
-    hipLaunchKernelGGL(positions_kernel, dim3((unsigned)((most + 255) / 256), (unsigned)images), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(positions_kernel, dim3(((unsigned)most + 255u) / 256u, (unsigned)images), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

@@ -23,3 +23,16 @@ def test_more_heads_than_a_launch_has_threads_for(tokens, heads, dim):
         want, _ = a.rotate(q[part], None, pos[part])
         assert torch.equal(out[part], want)
     a.close()
+
+
+def test_positions_of_as_many_tokens_as_an_index_counts():
+    """2^31 - 1 kept tokens: the launch's last threads have no token."""
+    kept = 2 ** 31 - 1
+    say("positions", kept)
+    idx = torch.zeros(kept, dtype=torch.int32, device=DEV)
+    T, H, W = 3, 17, 42107522
+    idx[-1] = T * H * W - 1
+    pos = tr.kept_positions(idx, [kept], [(T, H, W)], [(5, -6, 7)])
+    assert pos[:, -1].tolist() == [5 + T - 1, H - 1 - 6, 7 + W - 1]
+    for row, first in zip(pos, (5, -6, 7)):
+        assert (row[:-1] == first).all()
