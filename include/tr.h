@@ -442,7 +442,8 @@ tr_status tr_kept_positions(const int32_t* idx, int32_t B, const int32_t* K, con
 /* Norm and rotation of T tokens' heads: q [T, heads, head_dim] to q_out and
  * k [T, kv_heads, head_dim] to k_out (which may be q and k themselves); a NULL
  * q.p or k.p leaves that side out.  wq and wk: device [head_dim], or NULL
- * (required NULL without `norm`).  pos: device int32 [axes, ldpos], ldpos >= T. */
+ * (required NULL without `norm`).  pos: device int32, T positions of axis x at
+ * pos + x * ldpos (>= 0: 0 where all axes have the same ones, as text does). */
 tr_status tr_rotate(tr_attn* a, int64_t T, tr_heads q, tr_heads k, const void* wq, const void* wk,
                     const int32_t* pos, int64_t ldpos, tr_heads q_out, tr_heads k_out, void* stream);
 

@@ -201,8 +201,8 @@ class Attention:
             pos = pos[None]
         if pos.shape == (self.axes, tokens):
             row, unit = pos.stride()
-            if (unit == 1 or tokens <= 1) and (row >= tokens or self.axes == 1):
-                return pos.data_ptr(), max(row, tokens)
+            if unit == 1 or tokens <= 1:
+                return pos.data_ptr(), row
         raise ValueError("pos must be [%d, %d] with unit column stride, got %s" % (self.axes, tokens, tuple(pos.shape)))
 
     def _weight(self, name, w):

@@ -102,12 +102,12 @@ tr_status check_out_heads(const char* name, const tr_heads& x, int eb, int64_t T
     return TR_OK;
 }
 
-tr_status check_positions(const tr_attn* a, int64_t T, const int32_t* pos, int64_t ldpos)
+tr_status check_positions(const tr_attn* a, const int32_t* pos, int64_t ldpos)
 {
     if (!a->p.rot_dim) return TR_OK;
     if (!pos) return fail(TR_EINVAL, "pos must be non-NULL");
     if ((uintptr_t)pos & 3u) return fail(TR_EUNSUPPORTED, "pos must be 4-byte aligned");
-    if (a->p.axes > 1 && ldpos < T) return fail(TR_EINVAL, "ldpos = %lld must be >= T = %lld", (long long)ldpos, (long long)T);
+    if (a->p.axes > 1 && ldpos < 0) return fail(TR_EINVAL, "ldpos must be >= 0 (got %lld)", (long long)ldpos);
     return TR_OK;
 }
 
@@ -308,7 +308,7 @@ tr_status tr_rotate(tr_attn* a, int64_t T, tr_heads q, tr_heads k, const void* w
     if (k.p && ((st = check_heads("k", k, a->eb, T, a->p.kv_heads)) != TR_OK ||
                 (st = check_out_heads("k_out", k_out, a->eb, T, a->p.kv_heads, dim)) != TR_OK))
         return st;
-    if ((st = check_weights(a, wq, wk)) != TR_OK || (st = check_positions(a, T, pos, ldpos)) != TR_OK) return st;
+    if ((st = check_weights(a, wq, wk)) != TR_OK || (st = check_positions(a, pos, ldpos)) != TR_OK) return st;
     DeviceGuard g(a->device);
     if (!g.ok) return fail(TR_EDEVICE, "hipSetDevice(%d) failed", a->device);
     tr::RotateArgs r = rotate_args(a, T, wq, wk, pos, ldpos);
@@ -346,7 +346,7 @@ tr_status tr_rotate_backward(tr_attn* a, int64_t T, tr_heads gq, tr_heads gk, tr
                 (st = check_out_heads(name[i][2], *side[i][2], a->eb, T, heads, a->p.head_dim)) != TR_OK)
                 return st;
         }
-        if ((st = check_weights(a, wq, wk)) != TR_OK || (st = check_positions(a, T, pos, ldpos)) != TR_OK) return st;
+        if ((st = check_weights(a, wq, wk)) != TR_OK || (st = check_positions(a, pos, ldpos)) != TR_OK) return st;
     }
     if (T == 0 && !dwq && !dwk) return TR_OK;
     DeviceGuard g(a->device);
@@ -381,7 +381,7 @@ tr_status tr_append(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, c
     if (q.p && ((st = check_heads("q", q, a->eb, T, a->p.heads)) != TR_OK ||
                 (st = check_out_heads("q_out", q_out, a->eb, T, a->p.heads, dim)) != TR_OK))
         return st;
-    if ((st = check_weights(a, wq, wk)) != TR_OK || (st = check_positions(a, T, pos, ldpos)) != TR_OK) return st;
+    if ((st = check_weights(a, wq, wk)) != TR_OK || (st = check_positions(a, pos, ldpos)) != TR_OK) return st;
     DeviceGuard g(a->device);
     if (!g.ok) return fail(TR_EDEVICE, "hipSetDevice(%d) failed", a->device);
     tr::RotateArgs r = rotate_args(a, T, wq, wk, pos, ldpos);

@@ -36,3 +36,20 @@ def test_positions_of_as_many_tokens_as_an_index_counts():
     assert pos[:, -1].tolist() == [5 + T - 1, H - 1 - 6, 7 + W - 1]
     for row, first in zip(pos, (5, -6, 7)):
         assert (row[:-1] == first).all()
+
+
+def test_one_row_of_positions_for_all_axes():
+    """Text counts alike on every axis: an expanded row of positions."""
+    a = tr.Attention(4, 2, 64, BF, sections=(16, 8, 8), norm=True)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q, k = (torch.randn(50, h, 64, generator=g, device=DEV, dtype=BF) for h in (4, 2))
+    text = torch.arange(50, dtype=torch.int32, device=DEV)
+    whole, shared = text.expand(3, 50).contiguous(), text.expand(3, 50)
+    for want, got in zip(a.rotate(q, k, whole), a.rotate(q, k, shared)):
+        assert torch.equal(want, got)
+    for want, got in zip(a.rotate_backward(q, k, q, k, whole), a.rotate_backward(q, k, q, k, shared)):
+        assert torch.equal(want, got)
+    # and rows that overlap, as windows of one range do
+    windows = torch.arange(60, dtype=torch.int32, device=DEV).unfold(0, 50, 5)
+    for want, got in zip(a.rotate(q, k, windows.contiguous()), a.rotate(q, k, windows)):
+        assert torch.equal(want, got)
