@@ -357,7 +357,8 @@ tr_status tr_reduce_noalloc(const tr_params* p, const void* X, const void* X_pre
  * elements (i, i + rot_dim / 2), or (2 i, 2 i + 1) with `adjacent`:
  *   (a, b) -> (a cos z - b sin z, b cos z + a sin z),  z = pos[axis_i][t] freq_i.
  * z is the fp32 product of the position and the frequency, each rounded to fp32,
- * as models form it in training; its sine and cosine are right to fp32 at any z.
+ * as models form it in training; its sine and cosine are right to fp32 for |z| to
+ * 2^64.
  * Norm (with `norm`): x_j -> x_j w_j / sqrt(sum_j x_j^2 / head_dim + eps) over a
  * head, before its rotation; sums in fp32; a NULL weight is 1.
  *

@@ -2,8 +2,9 @@
 import pytest
 import torch
 
+import attn_ref as ref
 import paper_2607_13500_amd as tr
-from test_gpu_rotate import BF, DEV, say
+from test_gpu_rotate import BF, DEV, F32, UNIT, close, gen, say, values
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +54,16 @@ def test_one_row_of_positions_for_all_axes():
     windows = torch.arange(60, dtype=torch.int32, device=DEV).unfold(0, 50, 5)
     for want, got in zip(a.rotate(q, k, windows.contiguous()), a.rotate(q, k, windows)):
         assert torch.equal(want, got)
+
+
+def test_angles_up_to_2_to_the_64():
+    """Frequencies far above 1: fractions of a turn of angles that fp64 holds only to
+    whole turns."""
+    dim, inv = 32, [1.0, 3.7, 1e3, 12345.678, 1e5, 2.0 ** 20, 1e7, 1e8, 2.0 ** 30 + 1e3, 5e9, 8.5e9, -8.5e9, -1e6, 3e-9, 0.25, 7e9]
+    pos = torch.tensor([[1, -1, 2 ** 31 - 1, -2 ** 31, 123456789, 2 ** 30 + 12345, 1 << 24, 7, 99, 2000000011]], dtype=torch.int32)
+    a = tr.Attention(2, 2, dim, F32, inv_freq=inv)
+    q = values(gen(5), pos.shape[1], 2, dim, dtype=F32).to(DEV)
+    got, _ = a.rotate(q, None, pos.to(DEV))
+    x = q.cpu().double()
+    want = ref.turn(x, ref.angles(pos, inv, [0] * len(inv)), dim, False)
+    close(got, want, UNIT[F32], ref.pair_norm(x, dim, False), 3e-6, "large angles")
