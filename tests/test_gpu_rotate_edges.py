@@ -4,7 +4,7 @@ import torch
 
 import attn_ref as ref
 import paper_2607_13500_amd as tr
-from test_gpu_rotate import BF, DEV, F32, UNIT, close, gen, say, values
+from test_gpu_rotate import BF, DEV, F32, UNIT, close, freqs, gen, say, values
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,21 @@ def test_angles_up_to_2_to_the_64():
     x = q.cpu().double()
     want = ref.turn(x, ref.angles(pos, inv, [0] * len(inv)), dim, False)
     close(got, want, UNIT[F32], ref.pair_norm(x, dim, False), 3e-6, "large angles")
+
+
+def test_angles_are_those_of_positions_and_frequencies():
+    """The fp32 product stands for position times frequency: the position, the
+    frequency and the product are rounded by 2^-24 each, so the angle is off by less
+    than 3 * 2^-24 of itself, and an element by that of its pair's length."""
+    dim, rot = 64, 64
+    inv = freqs(rot)
+    pos = torch.cat([torch.arange(0, 40000, 37), torch.tensor([131071, 262143, 1048575])]).to(torch.int32)[None]
+    a = tr.Attention(1, 1, dim, F32)
+    q = values(gen(6), pos.shape[1], 1, dim, dtype=F32).to(DEV)
+    got, _ = a.rotate(q, None, pos.to(DEV))
+    x = q.cpu().double()
+    angle = pos[0].double()[:, None] * torch.tensor(inv, dtype=torch.float64)      # below 2^20: its 2^-53 are nothing here
+    want, length = ref.turn(x, angle, rot, False), ref.pair_norm(x, rot, False)
+    off = 3 * 2.0 ** -24 * torch.cat([angle, angle], 1)[:, None]
+    over = (got.cpu().double() - want).abs() - 2.0 ** -24 * want.abs() - (3e-6 + off) * length
+    assert float(over.max()) <= 0.0
