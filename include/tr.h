@@ -360,7 +360,8 @@ tr_status tr_reduce_noalloc(const tr_params* p, const void* X, const void* X_pre
  * as models form it in training; its sine and cosine are right to fp32 for |z| to
  * 2^64.
  * Norm (with `norm`): x_j -> x_j w_j / sqrt(sum_j x_j^2 / head_dim + eps) over a
- * head, before its rotation; sums in fp32; a NULL weight is 1.
+ * head, before its rotation; sums in fp32, of scaled elements where the squares
+ * themselves leave its range; a NULL weight is 1.
  *
  * Paged cache.  Token j of sequence b lies in page table[b][j / page_size], at
  * row j % page_size of it.  The new tokens are packed back to back; sequence b's

@@ -116,6 +116,13 @@ __device__ __forceinline__ float sum64(float x)
     return x;
 }
 
+// Heads whose mean square plus eps (v) leaves the range in which their fp32 squares
+// are right are taken again times a power of two: of squares past the largest fp32
+// times 2^-80, of tiny ones beside a tiny or no eps times 2^100.  v is then that of
+// the scaled head, and what is left of the scale goes into the gradient at its end.
+__device__ __forceinline__ bool in_range(float v) { return v >= 0x1p-100f && v <= 0x1.fffffep127f; }
+__device__ __forceinline__ float scale_for(float v) { return in_range(v) ? 1.f : v < 1.f ? 0x1p100f : 0x1p-80f; }
+
 // ---- any head: one wavefront a head, element by element -------------------------
 // Lane l holds pairs l and l + 64 (rot / 2 <= 128) and of the rest elements
 // rot + l + 64 j.
@@ -187,6 +194,18 @@ struct AnyHead {
 #pragma unroll
         for (int j = 0; j < kRest; ++j) r[j] = f(r[j], o.r[j]);
     }
+    // Takes the head times z, which scale_for chooses; 1 / sqrt(mean square + eps) of it.
+    __device__ __forceinline__ float inverse(const RotateArgs& g, float& z)
+    {
+        float v = dot(*this) / (float)g.dim + g.eps;
+        z = scale_for(v);
+        if (z != 1.f) {        // the whole wavefront's
+            const float f = z;
+            each(*this, [&](float p, float) { return p * f; });
+            v = dot(*this) / (float)g.dim + g.eps * f * f;
+        }
+        return 1.f / sqrtf(v);
+    }
     __device__ __forceinline__ void fill(float v)
     {
 #pragma unroll
@@ -232,7 +251,8 @@ __global__ __launch_bounds__(256) void rotate_any_kernel(RotateArgs g, int64_t f
             AnyHead<E> w;
             if (g.w[kind]) w.load(g, static_cast<const E*>(g.w[kind]), lane);
             else w.fill(1.f);
-            const float r = 1.f / sqrtf(x.dot(x) / (float)g.dim + g.eps);
+            float z;
+            const float r = x.inverse(g, z);
             x.each(w, [&](float v, float m) { return v * r * m; });
         }
         x.rotate(g, t, lane, false);
@@ -262,14 +282,15 @@ __global__ __launch_bounds__(256) void rotate_back_any_kernel(RotateArgs g)
         if (g.norm) x.load(g, static_cast<const E*>(g.in[kind].p) + t * g.in[kind].token + h * g.in[kind].head, lane);
         y.rotate(g, t, lane, true);
         if (g.norm) {
-            const float r = 1.f / sqrtf(x.dot(x) / (float)g.dim + g.eps);
+            float z;
+            const float r = x.inverse(g, z);
             x.each(x, [&](float v, float) { return v * r; });
             AnyHead<E> d = y;
             d.each(x, [](float p, float q) { return p * q; });
             dw.each(d, [](float p, float q) { return p + q; });
             y.each(w, [](float p, float q) { return p * q; });
             const float m = y.dot(x) / (float)g.dim;
-            y.each(x, [&](float p, float q) { return r * fmaf(-q, m, p); });
+            y.each(x, [&](float p, float q) { return r * fmaf(-q, m, p) * z; });
         }
         y.store(g, static_cast<E*>(g.out[kind].p) + t * g.out[kind].token + h * g.out[kind].head, lane);
     }
@@ -461,7 +482,7 @@ __device__ __forceinline__ Piece load_weight(const void* w, const Spot& sp)
     return p;
 }
 
-// 1 / sqrt(x), to within an ulp, for x of at least 2^-126.
+// 1 / sqrt(x), to within an ulp, for x of at least 2^-126 (in_range).
 __device__ __forceinline__ float rsqrt_(float x) { return __builtin_amdgcn_rsqf(x); }
 
 // Stores that nothing near reads again: past what the caches hold they are
@@ -534,7 +555,19 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int 
 #pragma unroll
                     for (int e = 0; e < kPiece; ++e) q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
                     q = group_sum<LP>(live ? q : 0.f);
-                    const float m = rsqrt_(fmaf(q, mean, g.eps));
+                    float v = fmaf(q, mean, g.eps);
+                    if (__any(live && !in_range(v))) {
+                        const float f = scale_for(v);
+                        q = 0.f;
+#pragma unroll
+                        for (int e = 0; e < kPiece; ++e) {
+                            x.a[e] *= f;
+                            x.b[e] *= f;
+                            q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
+                        }
+                        v = fmaf(group_sum<LP>(live ? q : 0.f), mean, g.eps * f * f);
+                    }
+                    const float m = rsqrt_(v);
                     const Piece& w = kind ? wk : wq;
 #pragma unroll
                     for (int e = 0; e < kPiece; ++e) {
@@ -634,7 +667,22 @@ __global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
                     }
                     q = group_sum<LP>(live ? q : 0.f);
                     m = group_sum<LP>(live ? m : 0.f);
-                    const float n = rsqrt_(fmaf(q, mean, g.eps));
+                    float v = fmaf(q, mean, g.eps), f = 1.f;
+                    const bool scaled = __any(live && !in_range(v));
+                    if (scaled) {
+                        f = scale_for(v);
+                        q = m = 0.f;
+#pragma unroll
+                        for (int e = 0; e < kPiece; ++e) {
+                            x.a[e] *= f;
+                            x.b[e] *= f;
+                            q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
+                            m = fmaf(y.a[e] * w.a[e], x.a[e], fmaf(y.b[e] * w.b[e], x.b[e], m));
+                        }
+                        v = fmaf(group_sum<LP>(live ? q : 0.f), mean, g.eps * f * f);
+                        m = group_sum<LP>(live ? m : 0.f);
+                    }
+                    const float n = rsqrt_(v);
                     m = m * n * mean;
 #pragma unroll
                     for (int e = 0; e < kPiece; ++e) {
@@ -643,6 +691,13 @@ __global__ __launch_bounds__(256) void rotate_back_kernel(RotateArgs g)
                         dw.b[e] += live ? y.b[e] * ub : 0.f;
                         y.a[e] = n * fmaf(-ua, m, y.a[e] * w.a[e]);
                         y.b[e] = n * fmaf(-ub, m, y.b[e] * w.b[e]);
+                    }
+                    if (scaled) {
+#pragma unroll
+                        for (int e = 0; e < kPiece; ++e) {
+                            y.a[e] *= f;
+                            y.b[e] *= f;
+                        }
                     }
                 }
                 if (live) {

@@ -4,7 +4,7 @@ import torch
 
 import attn_ref as ref
 import paper_2607_13500_amd as tr
-from test_gpu_rotate import BF, DEV, F32, UNIT, close, freqs, gen, say, values
+from test_gpu_rotate import BF, DEV, F32, UNIT, close, freqs, gen, inputs, positions, say, side64, values, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,43 @@ def test_angles_are_those_of_positions_and_frequencies():
     off = 3 * 2.0 ** -24 * torch.cat([angle, angle], 1)[:, None]
     over = (got.cpu().double() - want).abs() - 2.0 ** -24 * want.abs() - (3e-6 + off) * length
     assert float(over.max()) <= 0.0
+
+
+# ---- heads far from 1: squares beyond fp32, and below it -------------------------------
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("how", ["own", "odd"])
+@pytest.mark.parametrize("dim,adjacent", [(128, False), (64, True), (24, False), (256, True)])
+def test_norm_of_heads_of_every_size(dim, adjacent, how, dtype):
+    """Tolerances as in test_gpu_rotate: the norm does not depend on a head's size."""
+    sizes = torch.tensor([1.0, 1e-36, 1e25, 1e-19, 1e30, 1e-25, 3e18, 3e37, 1e-15, 1e19, 0.1])
+    for eps in (0.0, 1e-6, 1e-33):
+        say("sizes", dim, adjacent, how, dtype, eps)
+        g = gen(dim)
+        tokens, heads, kv_heads = len(sizes), 6, 2
+        a = tr.Attention(heads, kv_heads, dim, dtype, adjacent=adjacent, norm=True, eps=eps)
+        q, k = inputs(dim, dtype, tokens, heads, kv_heads, how, g)
+        order = torch.stack([sizes.roll(h) for h in range(heads)], 1)[..., None].to(DEV)      # other sizes beside each other
+        for x in (q, k):
+            x.copy_((torch.randn(x.shape, generator=g).clamp(-4, 4).to(DEV) * order[:, :x.shape[1]]).to(dtype))
+        wq, wk = weights(dim, dtype, g, True)
+        pos = positions(1, tokens, g)
+        for x, w, got in zip((q, k), (wq, wk), a.rotate(q, k, pos.to(DEV), wq=wq, wk=wk)):
+            want, _, ang, w64 = side64(x, w, pos, dim, dim, (dim // 2,), adjacent, True, eps)
+            unit = ref.norm(x.cpu().double(), w64, eps)
+            close(got, want, UNIT[dtype], ref.pair_norm(unit, dim, adjacent), 3e-6, eps)
+        # gradients, of heads whose own stay in the type's range
+        for x in (q, k):
+            size = order[:, :x.shape[1]].expand(x.shape)
+            x[(size < 1e-30) | (size > 2e30)] = 0.5
+        gq, gk = inputs(dim, dtype, tokens, heads, kv_heads, "own", g)
+        got = a.rotate_backward(gq, gk, q, k, pos.to(DEV), wq=wq, wk=wk)
+        for x, gr, w, dx, dw in ((q, gq, wq, got[0], got[2]), (k, gk, wk, got[1], got[3])):
+            _, _, ang, w64 = side64(x, w, pos, dim, dim, (dim // 2,), adjacent, True, eps)
+            x64, g64 = x.cpu().double(), gr.cpu().double()
+            want, want_w, mass = ref.backward(g64, x64, w64, ang, dim, adjacent, eps, True)
+            r = 1.0 / torch.sqrt((x64 * x64).mean(-1, keepdim=True) + eps)
+            gw = ref.turn(g64, -ang, dim, adjacent) * w64
+            scale = r * (ref.pair_norm(g64, dim, adjacent) * w64.abs() + (x64 * r).abs() * (gw * x64 * r).pow(2).mean(-1, keepdim=True).sqrt())
+            close(dx, want, UNIT[dtype], scale, 6e-6, eps)
+            close(dw, want_w, 0.0, mass, 5e-5, eps)
+        a.close()
