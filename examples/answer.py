@@ -99,26 +99,10 @@ def answer(layers, words, x, pos, lengths, tokens, room):
     return torch.stack(said)
 
 
-class Rotated(torch.autograd.Function):
-    """Normed and rotated queries and keys with their gradients."""
-
-    @staticmethod
-    def forward(ctx, attention, q, k, pos, wq, wk):
-        ctx.attention = attention
-        ctx.save_for_backward(q, k, pos, wq, wk)
-        return attention.rotate(q, k, pos, wq=wq, wk=wk)
-
-    @staticmethod
-    def backward(ctx, gq, gk):
-        q, k, pos, wq, wk = ctx.saved_tensors
-        dq, dk, dwq, dwk = ctx.attention.rotate_backward(gq.contiguous(), gk.contiguous(), q, k, pos, wq=wq, wk=wk)
-        return None, dq, dk, None, dwq.to(wq.dtype), dwk.to(wk.dtype)
-
-
 def train_step(attention, q, k, pos, wq, wk, target, rate=0.1):
     """One step of the norms' weights towards scores [heads, tokens, tokens]; the loss before it."""
     wq, wk = (w.detach().requires_grad_(True) for w in (wq, wk))
-    rq, rk = Rotated.apply(attention, q, k, pos, wq, wk)
+    rq, rk = attention.rotate(q, k, pos, wq=wq, wk=wk)
     rk = rk.repeat_interleave(attention.heads // attention.kv_heads, 1)
     scores = torch.matmul(rq.float().transpose(0, 1), rk.float().permute(1, 2, 0)) / math.sqrt(attention.head_dim)
     loss = (scores - target).square().mean()

@@ -2,8 +2,9 @@
 between the reduction and the model's answer (the tr_attn calls of include/tr.h).
 
 * kept_positions          - (time, height, width) of kept tokens in their image;
-* Attention.rotate        - norm of each head and rotation by position, one pass;
-* Attention.rotate_backward - its gradients;
+* Attention.rotate        - norm of each head and rotation by position, one pass,
+                            with a graph where its inputs have one;
+* Attention.rotate_backward - its gradients, for calls without autograd;
 * Attention.append        - the same on the way of new keys into a paged cache;
 * Attention.attend        - attention of the new tokens over that cache.
 
@@ -116,6 +117,31 @@ def kept_positions(idx: torch.Tensor, K: Sequence[int], grid: Sequence[Tuple[int
             status = lib.tr_kept_positions(*args, handle)
     _check(status, "tr_kept_positions")
     return out
+
+
+class _Rotated(torch.autograd.Function):
+    """Attention.rotate with a graph."""
+
+    @staticmethod
+    def forward(ctx, attention, q, k, pos, wq, wk):
+        ctx.attention, norm = attention, attention.norm
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(q if norm else None, k if norm else None, pos, wq, wk)
+        return attention._rotate(q, k, pos, wq, wk, None, None, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, *g):
+        q, k, pos, wq, wk = ctx.saved_tensors
+        _, need_q, need_k, _, need_wq, need_wk = ctx.needs_input_grad
+        # an expanded gradient (of a sum) has no unit stride
+        gq, gk = (x if x is None or x.stride(-1) == 1 else x.contiguous() for x in g)
+        gq, gk = gq if need_q or need_wq else None, gk if need_k or need_wk else None
+        if gq is None and gk is None:
+            return (None,) * 6
+        dq, dk, dwq, dwk = ctx.attention.rotate_backward(gq, gk, q, k, pos, wq=wq, wk=wk)
+        dwq, dwk = (d.to(w.dtype) if need and d is not None else None for d, w, need in ((dwq, wq, need_wq), (dwk, wk, need_wk)))
+        return None, dq if need_q else None, dk if need_k else None, None, dwq, dwk
 
 
 class Attention:
@@ -244,8 +270,20 @@ class Attention:
                wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
         """(q_out, k_out): heads q [tokens, heads, head_dim] and k [tokens,
-        kv_heads, head_dim] normed (with norm) and rotated to pos [axes, tokens].
-        Either may be None; the outputs may be the inputs themselves."""
+        kv_heads, head_dim] normed (with norm) and rotated to pos [axes, tokens]
+        (rows may coincide: text.expand(axes, -1)).  Either may be None; the
+        outputs may be the inputs themselves.  Where autograd records and q, k or
+        a weight requires a gradient, the outputs are the call's own and have one."""
+        if torch.is_grad_enabled():
+            for t in (q, k, wq, wk):
+                if t is not None and t.requires_grad:
+                    if q_out is not None or k_out is not None:
+                        raise RuntimeError("q_out and k_out take no gradient: leave them out, or call rotate without recording")
+                    with torch.cuda.stream(stream):      # the gradient's stream too
+                        return _Rotated.apply(self, q, k, pos, wq, wk)
+        return self._rotate(q, k, pos, wq, wk, q_out, k_out, stream)
+
+    def _rotate(self, q, k, pos, wq, wk, q_out, k_out, stream):
         if q is None and k is None:
             raise ValueError("nothing to rotate")
         tokens = (q if q is not None else k).shape[0]
@@ -295,7 +333,8 @@ class Attention:
                q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
         """rotate for the new tokens of a step: their keys go to their place in
         the cache, their values (as they are) beside them; returns q_out (None
-        where q is).  Slices of one projection's output are fine."""
+        where q is).  Slices of one projection's output are fine.  Passes no
+        gradient."""
         tokens = k.shape[0]
         hk, hv = self._heads("k", k, self.kv_heads, tokens), self._heads("v", v, self.kv_heads, tokens)
         hq = oq = _NONE
@@ -318,7 +357,7 @@ class Attention:
         `window` of them; otherwise all kv_len tokens of its sequence.  A row
         that sees none is 0 with lse = -inf.  scale is 1 / sqrt(head_dim) unless
         given.  lse (float32 [tokens, heads], natural logarithm) is None unless
-        wanted.
+        wanted.  Passes no gradient.
         """
         tokens = q.shape[0]
         hq = self._heads("q", q, self.heads, tokens)
