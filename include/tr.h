@@ -415,7 +415,7 @@ typedef struct {
 typedef struct {
     int32_t seqs;
     int32_t table_width;      /* pages in a row of table                            */
-    int64_t table_stride;     /* entries from one row of table to the next          */
+    int64_t table_stride;     /* entries from one row of table to the next, >= 0    */
     const int32_t* q_start;   /* device [seqs + 1]                                  */
     const int32_t* kv_len;    /* device [seqs], with the new tokens                 */
     const int32_t* table;     /* device [seqs, table_width]                         */

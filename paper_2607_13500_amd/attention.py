@@ -261,8 +261,7 @@ class Attention:
             seqs, (rows, width), (row, unit) = kv_len.shape[0], table.shape, table.stride()
             if q_start.shape == (seqs + 1,) and rows == seqs and (unit == 1 or width <= 1) and q_start.is_contiguous() \
                     and kv_len.is_contiguous():
-                return StepArgs(seqs, width, row if seqs > 1 else max(row, width), q_start.data_ptr(), kv_len.data_ptr(),
-                                table.data_ptr())
+                return StepArgs(seqs, width, row, q_start.data_ptr(), kv_len.data_ptr(), table.data_ptr())
         raise ValueError("step must hold q_start [seqs + 1], kv_len [seqs] and table [seqs, width], rows contiguous")
 
     # -- the operators ------------------------------------------------------

@@ -141,9 +141,9 @@ tr_status check_cache(const tr_attn* a, const tr_cache* c, const tr_step* s)
         return fail(TR_EINVAL, "the cache has rows that overlap (strides %lld, %lld and %lld, rows of %lld elements)",
                     (long long)c->page, (long long)c->token, (long long)c->head, (long long)dim);
     if (s->seqs < 1) return fail(TR_EINVAL, "seqs must be >= 1 where there are tokens (got %d)", s->seqs);
-    if (s->table_width < 0 || s->table_stride < s->table_width)
-        return fail(TR_EINVAL, "table_stride = %lld must be >= table_width = %d >= 0", (long long)s->table_stride,
-                    s->table_width);
+    if (s->table_width < 0 || s->table_stride < 0)
+        return fail(TR_EINVAL, "table_width = %d and table_stride = %lld must be >= 0", s->table_width,
+                    (long long)s->table_stride);
     if (!s->q_start || !s->kv_len || (!s->table && s->table_width))
         return fail(TR_EINVAL, "q_start, kv_len and table must be non-NULL");
     if (((uintptr_t)s->q_start | (uintptr_t)s->kv_len | (uintptr_t)s->table) & 3u)

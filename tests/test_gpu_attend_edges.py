@@ -204,3 +204,18 @@ def test_more_items_than_a_launch_has_threads_for():
     for t in range(0, tokens, 4096):
         assert (out[t:t + 4096] == want[t:t + 4096, None, None]).all()
     a.close()
+
+
+def test_one_row_of_the_table_for_all_sequences():
+    """Sequences that read the same pages: an expanded row, which is only read."""
+    g = gen(9)
+    for heads, kv_heads, new in ((4, 2, [1, 1, 1]), (8, 1, [20, 3, 9])):
+        table = torch.tensor([[2, 0, 3]], dtype=torch.int32)
+        whole = tr.Step(torch.tensor([0] + [sum(new[:b + 1]) for b in range(3)], dtype=torch.int32),
+                        torch.tensor([40, 33, 45], dtype=torch.int32), table.expand(3, 3).contiguous())
+        cache, q = normal_caches(4, 16, kv_heads, 64, g), torch.randn(sum(new), heads, 64, generator=g).to(BF).to(DEV)
+        a = tr.Attention(heads, kv_heads, 64, BF)
+        want, _ = a.attend(q, cache, on_device(whole))
+        shared = on_device(whole)._replace(table=table.to(DEV).expand(3, 3))
+        assert shared.table.stride(0) == 0 and torch.equal(a.attend(q, cache, shared)[0], want)
+        a.close()
