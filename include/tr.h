@@ -421,9 +421,13 @@ typedef struct {
     const int32_t* table;     /* device [seqs, table_width]                         */
 } tr_step;
 
-/* A layer's geometry on the current device, with the scratch of its calls
- * (12 MB at head_dim 128): as with a tr_ctx, one stream at a time.  Errors as
- * tr_create. */
+/* A layer's geometry on the current device, with the scratch of its calls: at 256
+ * compute units 1 MB or less for gradients and, where tr_attend can be called
+ * (bf16, head_dim a multiple of 8), 35 MB up to head_dim 64 and 68 MB above.
+ * Layers of one geometry can share a context.  As with a tr_ctx, one stream at a
+ * time: two tr_attend (or tr_rotate_backward) calls of a context that overlap
+ * take each other's parts, and what the first two leave there can make later
+ * tr_attend calls of that context wrong.  Errors as tr_create. */
 tr_status tr_attn_create(const tr_attn_params* p, tr_attn** out);
 void tr_attn_destroy(tr_attn* a);
 
@@ -434,7 +438,8 @@ void tr_attn_destroy(tr_attn* a);
  *   idx    device int32 [sum K], image-local (tr_reduce's out_idx)
  *   K      host [B], >= 0 kept tokens of each image
  *   grid   host [B, 3], each >= 1, and start host [B, 3]
- *   dst    host [B] or NULL; image b's columns must end within ldpos
+ *   dst    host [B] or NULL; image b's columns must end within ldpos, and none
+ *          belong to two images
  *   pos    device int32 [3, ldpos] (other columns stay as they are)
  * Needs no context. */
 tr_status tr_kept_positions(const int32_t* idx, int32_t B, const int32_t* K, const int32_t* grid,

@@ -154,6 +154,11 @@ class Attention:
     one axis.  adjacent pairs are elements (2 i, 2 i + 1), otherwise
     (i, i + rot_dim / 2).  norm: heads are divided by their root mean square
     (eps added to its square) and multiplied by a weight before they rotate.
+
+    Layers of one geometry can share an Attention: it holds no weights, only the
+    scratch of rotate_backward and attend (up to 68 MB).  That scratch is for one
+    stream (and one thread) at a time: a call on another stream has to wait for
+    those before it, by an event or wait_stream.
     """
 
     def __init__(self, heads: int, kv_heads: Optional[int] = None, head_dim: int = 128,

@@ -13,7 +13,9 @@
 // transposing reads of shared memory.
 //
 // Weights are rounded to bf16 for the second product (the sum l takes them
-// unrounded): its operands have one type, and V is bf16.
+// unrounded): its operands have one type, and V is bf16.  A second product with
+// what the rounding leaves, for which few rows have the time, would turn infinite
+// values into NaN: that rest is 0 or negative as often as not.
 #include <algorithm>
 
 #include "tr_attn.h"
@@ -145,8 +147,9 @@ __device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b)
     return (int64_t)tiles_of<ROWS>(a, s) * steps_of<STEP>(s) * a.kv_heads;
 }
 
-// All steps, and a workgroup's share of them.  An item has at most kMostParts
-// parts, which one workgroup can join.
+// All steps, and a workgroup's share of them: at least 1 / kMostParts of the
+// longest item's, so that an item, which may begin inside a share, has at most
+// kMostParts + 1 parts, which one workgroup can join.
 constexpr int kMostParts = 64;
 
 struct Shares {
