@@ -182,13 +182,20 @@ __device__ __forceinline__ Shares shares_of(const AttendArgs& a, int lane)
     return r;
 }
 
-// The sequence that step u (< all_steps) lies in.
+// Sequences up to which a workgroup may look for an item among all of them, a wavefront
+// 64 at a time, instead of walking over those of its share (8 heads of keys of 128,
+// a group of 4; 64 sequences of 128 tokens over 512: 135 us by items, 148 by shares;
+// 256 of 64: 333 and 321; 1024 of 16: 1027 and 770; 16384 of 16 over 64: 69 and 4.4 ms).
+constexpr int kSearched = 128;
+
+// The sequence that step u (< all_steps) lies in, searched from sequence `from`
+// on, before which lie `before` (<= u) steps: a workgroup walks the sequences of
+// its share once.
 template <int ROWS, int STEP>
-__device__ __forceinline__ Place place_of(const AttendArgs& a, int64_t u, int lane)
+__device__ __forceinline__ Place place_of(const AttendArgs& a, int64_t u, int lane, int from = 0, int64_t before = 0)
 {
     Place p{};
-    int64_t before = 0;
-    for (int b0 = 0; b0 < a.step.seqs; b0 += 64) {
+    for (int b0 = from; b0 < a.step.seqs; b0 += 64) {
         const int64_t c = cost_of<ROWS, STEP>(a, b0 + lane);
         int64_t sum = c;
 #pragma unroll
@@ -351,8 +358,12 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
     int64_t u = (int64_t)blockIdx.x * all.share;
     const int64_t u_end = min(u + all.share, all.total);
 
+    int from = 0;
+    int64_t before = 0;
     while (u < u_end) {
-        const Place pl = place_of<kRows, kStep>(a, u, lane);
+        const Place pl = place_of<kRows, kStep>(a, u, lane, from, before);
+        from = pl.b;
+        before = pl.first;
         const Sequence s = pl.s;
         const int64_t local = u - pl.first;
         const int item = (int)(local / pl.steps), step0 = (int)(local - (int64_t)item * pl.steps);
@@ -679,7 +690,7 @@ __device__ __forceinline__ bool items_alone(const AttendArgs& a, const Shares& a
 {
     if constexpr (STEP == 0) return true;
     else {
-        if (!a.causal) return false;
+        if (!a.causal || a.step.seqs > kSearched) return false;
         float sum = 0.f, most = 0.f;
         const float tile = (float)(ROWS / a.group + 1);             // new tokens of a tile
         for (int b = lane; b < a.step.seqs; b += 64) {
@@ -757,8 +768,12 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend_many_kernel
         for (int i = threadIdx.x; i < 4 * BYTES / 16; i += T) reinterpret_cast<u32x4*>(smem)[i] = u32x4{};   // pieces past the head stay zero
         __syncthreads();
     }
+    int from = 0;
+    int64_t before = 0;
     while (by_item ? u >= 0 : u < u_end) {
-        const Place pl = by_item ? place_of<ROWS, 0>(a, u, lane) : place_of<ROWS, STEP>(a, u, lane);
+        const Place pl = by_item ? place_of<ROWS, 0>(a, u, lane) : place_of<ROWS, STEP>(a, u, lane, from, before);
+        from = pl.b;
+        before = pl.first;
         const Sequence s = pl.s;
         const int64_t local = u - pl.first;
         const int item = (int)(local / pl.steps), step0 = (int)(local - (int64_t)item * pl.steps);
@@ -1120,7 +1135,7 @@ hipError_t many(const AttendArgs& a, hipStream_t s)
     // chunks of 256 tokens over 4000: 398 us by items, 416 by shares; 1024: 693 and
     // 761; 128: 159 and 145; shares also keep a long context among short ones from
     // being one workgroup's).  A launch has fewer than 2^32 threads.
-    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus && items * (NW * 64) <= (int64_t)UINT32_MAX) {
+    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus && a.step.seqs <= kSearched && items * (NW * 64) <= (int64_t)UINT32_MAX) {
         if (a.dim == DH) return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, true>, items) : launch(attend_many_kernel<DH, NW, 0, false, true>, items);
         return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, false>, items) : launch(attend_many_kernel<DH, NW, 0, false, false>, items);
     }

@@ -186,15 +186,17 @@ def test_scale_zero_of_queries_that_are_not_finite(kernel):
     a.close()
 
 
-def test_more_items_than_a_launch_has_threads_for():
+@pytest.mark.parametrize("seqs,kv_heads,tokens", [(1000, 1, 32766), (128, 65535, 4200)])
+def test_more_items_than_a_launch_has_threads_for(seqs, kv_heads, tokens):
     """2^23 tiles of 256 rows and more, of 512 threads each.  Keys of zeros and equal
     values, so that every row of a sequence is its value exactly."""
-    seqs, heads, dim, tokens, page_size = 1000, 65535, 8, 32766, 16
-    say("large", seqs, heads, tokens)
-    a = tr.Attention(heads, 1, dim, BF)
-    assert (tokens * heads + seqs * 256) * 2 >= 2 ** 32
+    heads, dim, page_size = 65535, 8, 16
+    say("large", seqs, heads, kv_heads, tokens)
+    a = tr.Attention(heads, kv_heads, dim, BF)
+    assert (tokens * heads // kv_heads + seqs * 256) * kv_heads * 2 >= 2 ** 32
     value = (torch.arange(seqs, device=DEV) % 200 + 1).to(BF)
-    cache = tr.KVCache(torch.zeros(seqs, page_size, 1, dim, dtype=BF, device=DEV), value[:, None, None, None].expand(seqs, page_size, 1, dim).contiguous())
+    shape = (seqs, page_size, kv_heads, dim)
+    cache = tr.KVCache(torch.zeros(shape, dtype=BF, device=DEV), value[:, None, None, None].expand(shape).contiguous())
     q_start = (torch.arange(seqs + 1, device=DEV) * tokens // seqs).to(torch.int32)
     step = tr.Step(q_start, torch.full((seqs,), 11, dtype=torch.int32, device=DEV), torch.arange(seqs, dtype=torch.int32, device=DEV)[:, None])
     q = torch.ones(1, 1, dim, dtype=BF, device=DEV).expand(tokens, heads, dim)
@@ -219,3 +221,43 @@ def test_one_row_of_the_table_for_all_sequences():
         shared = on_device(whole)._replace(table=table.to(DEV).expand(3, 3))
         assert shared.table.stride(0) == 0 and torch.equal(a.attend(q, cache, shared)[0], want)
         a.close()
+
+
+def singles(seqs, new, g, heads=4, kv_heads=2, dim=64, page_size=16, kv=16):
+    """`seqs` sequences of `new` tokens at the end of a page of their own."""
+    cache = tr.KVCache(*(torch.randn(seqs, page_size, kv_heads, dim, generator=g, device=DEV, dtype=BF) for _ in range(2)))
+    step = tr.Step(torch.arange(seqs + 1, dtype=torch.int32, device=DEV) * new, torch.full((seqs,), kv, dtype=torch.int32, device=DEV),
+                   torch.randperm(seqs, device=DEV, generator=g).to(torch.int32)[:, None])
+    return torch.randn(seqs * new, heads, dim, generator=g, device=DEV, dtype=BF), cache, step
+
+
+@pytest.mark.parametrize("new", [1, 16])
+def test_thousands_of_sequences(new):
+    """Every workgroup walks over the sequences once: the time of a call grows with
+    their number, not with its square (four times as many: 4, not 16 times)."""
+    g = torch.Generator(device=DEV).manual_seed(new)
+    heads, kv_heads, dim = (4, 2, 64) if new == 1 else (16, 2, 64)
+    times = []
+    for seqs in (5003, 20012):
+        say("sequences", seqs, new)
+        q, cache, step = singles(seqs, new, g, heads, kv_heads, dim)
+        a = tr.Attention(heads, kv_heads, dim, BF)
+        out, _ = a.attend(q, cache, step)
+        k, v = (c[step.table[:, 0].long()].double().repeat_interleave(heads // kv_heads, 2) for c in cache)      # [seqs, 16, heads, dim]
+        for i in range(new):
+            s = (q[i::new].double()[:, None] * k).sum(-1) / math.sqrt(dim)
+            s[:, 16 - new + i + 1:] = -math.inf
+            w = torch.softmax(s, 1)[..., None]
+            want, mass = (w * v).sum(1), (w * v.abs()).sum(1)
+            assert float(((out[i::new].double() - want).abs() - 2.0 ** -8 * want.abs() - (2.0 ** -8 + 1.5e-3) * mass).max()) <= 0.0
+        least = math.inf
+        for _ in range(5):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            a.attend(q, cache, step, out=out)
+            end.record()
+            torch.cuda.synchronize()
+            least = min(least, begin.elapsed_time(end))
+        times.append(least)
+        a.close()
+    assert times[1] < 9 * times[0], times
