@@ -167,7 +167,7 @@ __device__ __forceinline__ Shares shares_of(const AttendArgs& a, int lane)
             const Sequence s = sequence_at(a, b);
             const int steps = steps_of<STEP>(s);
             sum += (int64_t)tiles_of<ROWS>(a, s) * steps * a.kv_heads;
-            most = max(most, steps);
+            if (s.n > 0) most = max(most, steps);       // those without new tokens have no items
         }
     }
 #pragma unroll

@@ -231,6 +231,18 @@ def singles(seqs, new, g, heads=4, kv_heads=2, dim=64, page_size=16, kv=16):
     return torch.randn(seqs * new, heads, dim, generator=g, device=DEV, dtype=BF), cache, step
 
 
+def least_time(call):
+    least = math.inf
+    for _ in range(5):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        call()
+        end.record()
+        torch.cuda.synchronize()
+        least = min(least, begin.elapsed_time(end))
+    return least
+
+
 @pytest.mark.parametrize("new", [1, 16])
 def test_thousands_of_sequences(new):
     """Every workgroup walks over the sequences once: the time of a call grows with
@@ -250,14 +262,29 @@ def test_thousands_of_sequences(new):
             w = torch.softmax(s, 1)[..., None]
             want, mass = (w * v).sum(1), (w * v.abs()).sum(1)
             assert float(((out[i::new].double() - want).abs() - 2.0 ** -8 * want.abs() - (2.0 ** -8 + 1.5e-3) * mass).max()) <= 0.0
-        least = math.inf
-        for _ in range(5):
-            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
-            begin.record()
-            a.attend(q, cache, step, out=out)
-            end.record()
-            torch.cuda.synchronize()
-            least = min(least, begin.elapsed_time(end))
-        times.append(least)
+        times.append(least_time(lambda: a.attend(q, cache, step, out=out)))
         a.close()
     assert times[1] < 9 * times[0], times
+
+
+def test_a_long_sequence_without_new_tokens():
+    """A slot that waits, however long its context, takes nothing from the others: the
+    same rows, and their work still goes to all workgroups."""
+    say("waiting")
+    g = gen(10)
+    kv, waiting, page_size = 20000, 1 << 20, 64
+    cache, q = normal_caches(320, page_size, 8, 128, g), torch.randn(1, 8, 128, generator=g).to(BF).to(DEV)
+    table = torch.zeros(2, waiting // page_size, dtype=torch.int32)
+    table[0, :320] = torch.randperm(320, generator=g)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    alone = tr.Step(i32([0, 1]), i32([kv]), table[:1].to(DEV))
+    both = tr.Step(i32([0, 1, 1]), i32([kv, waiting]), table.to(DEV))
+    a = tr.Attention(8, 8, 128, BF)
+    want, _ = a.attend(q, cache, alone)
+    got, _ = a.attend(q, cache, both)
+    # other parts, other roundings: each is within its bound of the definition
+    ref_out, _, mass, _ = definition(q, cache, tr.Step(*(t.cpu() for t in alone)), 128 ** -0.5, True)
+    for out in (want, got):
+        assert float(((out.double() - ref_out).abs() - 2.0 ** -8 * ref_out.abs() - (2.0 ** -8 + 1.5e-3) * mass).max()) <= 0.0
+    assert least_time(lambda: a.attend(q, cache, both)) < 3 * least_time(lambda: a.attend(q, cache, alone))
+    a.close()
