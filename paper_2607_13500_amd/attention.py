@@ -25,7 +25,7 @@ from . import _lib
 from ._lib import AttnParams, Cache, Heads, StepArgs
 
 # Small calls are bound by this module's own work (one decoded token: 9 us a call
-# against 15 us on the device), so each tensor is looked at once, devices are
+# against 12.5 us on the device), so each tensor is looked at once, devices are
 # compared as indices, and streams are asked for as plain handles.
 
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") \

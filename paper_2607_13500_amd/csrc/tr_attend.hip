@@ -659,9 +659,10 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
 // 64 that go from memory straight into shared memory, two tiles there at a time:
 // one is loaded while the other is worked on.  Bound by the matrix instructions
 // and by the softmax between them, which the two wavefronts of a SIMD overlap:
-// a prompt of 18432 tokens of 32 heads of 128 takes 2.82-2.92 ms (953-988
-// TFLOP/s; 42 % of the matrix units' cycles), eight chunks over long contexts
-// 550 us (660: the last shares end unevenly, and their parts are joined).
+// a prompt of 18432 tokens of 32 heads of 128 takes 2.85-3.01 ms by the box
+// (925-977 TFLOP/s; 42 % of the matrix units' cycles), eight chunks over long
+// contexts 530-565 us (640-684: the last shares end unevenly, and their parts are
+// joined).
 //
 // Shared memory rows are DH elements in pieces of 16 bytes; piece c of row r lies
 // at piece c ^ f(r), which the loads bring about by each lane's choice of source
@@ -683,7 +684,7 @@ __device__ __forceinline__ int v_swizzle(int row)
 // window, little more than it) the shares of such tiles are done sooner.  Taken
 // whole, the steps of the tiles themselves count, and half of the longest tile's
 // at the end while other workgroups have none left.  8 heads of keys, a group of 4:
-// a prompt of 3800 tokens from an empty cache takes 214 us so and 306 by shares,
+// a prompt of 3800 tokens from an empty cache takes 199 us so and 296 by shares,
 // 1500 tokens with a window of 512 over 8000 37 and 65.
 template <int ROWS, int STEP>
 __device__ __forceinline__ bool items_alone(const AttendArgs& a, const Shares& all, int lane)
@@ -1094,7 +1095,7 @@ Divisor divisor(uint32_t d)
 
 // Whether 16 tokens from a multiple of 16 on lie in one page of less than 2 GB.
 // Addressing them by the wavefront takes 64 single tokens over 8000 (pages of 64)
-// from 181 to 175 us and a prompt of 8192 from 628 to 612.
+// from 178 to 173 us; a prompt of 8192 takes 599 either way.
 bool in_halves(const AttendArgs& a)
 {
     return a.cache.page_size % 16 == 0 && a.cache.token < INT32_MAX / 2 && a.cache.token * 2 * (int64_t)a.cache.page_size < INT32_MAX;
@@ -1132,8 +1133,8 @@ hipError_t many(const AttendArgs& a, hipStream_t s)
     const bool pg16 = in_halves(a);
     // An item a workgroup where that makes two rounds at least, else a workgroup a CU
     // and shares of the steps (8 heads of keys of 128, a group of 4; 512 items of
-    // chunks of 256 tokens over 4000: 398 us by items, 416 by shares; 1024: 693 and
-    // 761; 128: 159 and 145; shares also keep a long context among short ones from
+    // chunks of 256 tokens over 4000: 349 us by items, 357 by shares; 1024: 639 and
+    // 677; 128: 143 and 103; shares also keep a long context among short ones from
     // being one workgroup's).  A launch has fewer than 2^32 threads.
     if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus && a.step.seqs <= kSearched && items * (NW * 64) <= (int64_t)UINT32_MAX) {
         if (a.dim == DH) return pg16 ? launch(attend_many_kernel<DH, NW, 0, true, true>, items) : launch(attend_many_kernel<DH, NW, 0, false, true>, items);
@@ -1152,8 +1153,8 @@ hipError_t attend(const AttendArgs& args, hipStream_t s)
 {
     AttendArgs a = args;
     // By the rows of a sequence and key head, on average (28 and 4 heads of 128, 16
-    // contexts of 8000): 28 rows take 97 us as few and 119 as many, 35 rows 136 and
-    // 125; 64 contexts of 2000: 89 and 93, 133 and 96.
+    // contexts of 8000): 28 rows take 98 us as few and 121 as many, 35 rows 137 and
+    // 125; 64 contexts of 2000: 88 and 92, 132 and 95.
     if (a.tokens * a.group <= 32 * (int64_t)a.step.seqs) {
         a.scale = a.raw_scale * kLog2e;
         return few<DH>(a, s);

@@ -12,10 +12,10 @@
 //
 // All of it is bound by memory: heads are read once and written once.  Measured:
 // 36864 tokens of 40 bf16 heads of 128 in 132-138 us (5.5-5.7 TB/s read and
-// written; a library copy of 2 GiB 5.0), 8 prompts appended (9000 tokens) in 36 us
-// (5.3), gradients of 16384 tokens in 93 us (5.4) and the sum of dw in 5 more.
-// Small calls are bound by their launch: 64 tokens appended 5.4 us, 577 fp32 tokens
-// 5.3, positions of 64 clips 2.7.
+// written; a library copy of 2 GiB 5.0), 8 prompts appended (9000 tokens) in 37 us
+// (5.2), gradients of 16384 tokens in 93 us (5.4) and the sum of dw in 5 more.
+// Small calls are bound by their launch: 64 tokens appended 5.6 us, 577 fp32 tokens
+// 6.1, positions of 64 clips 2.6.
 #include <algorithm>
 #include <type_traits>
 
