@@ -67,6 +67,7 @@
 #ifndef TR_H
 #define TR_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -352,6 +353,9 @@ tr_status tr_reduce_noalloc(const tr_params* p, const void* X, const void* X_pre
  *   tr_rotate_backward  its gradients
  *   tr_append           the same on the way of new keys into a paged cache
  *   tr_attend           attention of the new tokens over that cache
+ *   tr_append8, tr_attend8   the same on a cache of 8-bit values
+ *   tr_update_pages     tables, row starts, slots and positions of a step
+ *   tr_verify_drafts    drafted tokens against the target's probabilities
  *
  * Rotation.  The first rot_dim elements of a head turn in pairs, pair i being
  * elements (i, i + rot_dim / 2), or (2 i, 2 i + 1) with `adjacent`:
@@ -486,6 +490,110 @@ tr_status tr_append(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, c
 tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const tr_step* s,
                     double scale, int32_t causal, int32_t window, tr_heads out, float* lse,
                     void* stream);
+
+/* A paged cache of 8-bit values (e4m3: 1 sign, 4 exponent and 3 mantissa bits, no
+ * infinities, largest value 448) with a fp32 scale for each block of `block` tokens
+ * of a page and key head: row r of page g stands for k times
+ * k_scale[g * scale_page + (r / block) * scale_block + h * scale_head], v likewise.
+ * Strides of k and v in elements (bytes), of the scales in floats. */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    int32_t pages;
+    int32_t page_size;
+    int32_t block;            /* divides page_size */
+    int64_t page;
+    int64_t token;
+    int64_t head;
+    int64_t scale_page;
+    int64_t scale_block;
+    int64_t scale_head;
+} tr_cache8;
+
+/* tr_append into a cache of 8-bit values (fp32 and bf16 contexts).  Each block, key
+ * head and side (keys, values) takes the smallest scale 2^e, -117 <= e <= 120, with
+ * which its new tokens' largest finite element lies within 448 2^e; where the block
+ * holds older tokens of the sequence their scale stays if it is large enough, else
+ * they are rounded again with the new one.  Elements are fp32 until they are rounded
+ * to e4m3, to the nearest, ties to even; one that is not finite becomes NaN.  A
+ * sequence's new tokens must not share a block with another's.  (A scale of older
+ * tokens need not be a power of two, but finite and > 0.) */
+tr_status tr_append8(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, const void* wq,
+                     const void* wk, const int32_t* pos, int64_t ldpos, tr_heads q_out,
+                     const tr_cache8* c, const tr_step* s, void* stream);
+
+/* tr_attend over a cache of 8-bit values (bf16 contexts only); scales are finite and
+ * >= 0 where a row sees their tokens.  Keys' scales multiply scores and values'
+ * scales weights, in fp32, before these are rounded to bf16.
+ * head_dim must be a multiple of 16, and q's, out's and the cache's bases and
+ * strides of 16 bytes, else TR_EUNSUPPORTED. */
+tr_status tr_attend8(tr_attn* a, int64_t T, tr_heads q, const tr_cache8* c, const tr_step* s,
+                     double scale, int32_t causal, int32_t window, tr_heads out, float* lse,
+                     void* stream);
+
+/* Free pages: a ring of page numbers, state[1] of them from index state[0] on
+ * (modulo pages).  Pages are taken from the front and given back to the end. */
+typedef struct {
+    int32_t pages;            /* of the cache, and entries of ring: >= 1 */
+    int32_t* ring;            /* device [pages] */
+    const int32_t* state;     /* device [2]: index of the first free page, free pages */
+    int32_t* state_out;       /* device [2], may be state itself */
+} tr_pool;
+
+/* A step's tables from the sequences' lengths: sequence b grows by change[b] new
+ * tokens, or gives up its last -change[b] (all of them where it has fewer), and
+ * takes or gives back pages so that it holds ceil(length / page_size):
+ *   kv_out[b]   = max(kv_len[b] + change[b], 0)                (may be kv_len itself)
+ *   table       pages taken behind those that the sequence holds, from the pool's
+ *               front, sequence by sequence; those given back go to the pool's end,
+ *               sequence by sequence in the order of the table (their entries stay),
+ *               and are not taken in the same call
+ *   q_start[b]  = sum of max(change, 0) over the sequences before b    [seqs + 1]
+ *   slots, pos  for each of the rows packed rows: page * page_size + row in the cache
+ *               (int64) and the place in the sequence (int32); rows that belong to no
+ *               sequence get -1 and 0.  Either may be NULL.
+ *   short_of    0; or the number of pages that the pool lacks; or 2^31 - 1 where a
+ *               sequence outgrows its row of the table, or the new tokens the rows.
+ *               Then nothing else changes: kv_out and state_out are kv_len and
+ *               state, q_start is 0 throughout, slots -1 and pos 0.
+ * All pointers are device memory, so a step recorded in a HIP graph replays with
+ * what they hold then.  kv_len must be >= 0, state within the ring, and a page held
+ * by one sequence only; what is outside is never followed, and its results are
+ * unspecified.  Needs no context. */
+tr_status tr_update_pages(int32_t seqs, const int32_t* change, const int32_t* kv_len, int32_t* kv_out,
+                          int32_t* table, int32_t table_width, int64_t table_stride, int32_t page_size,
+                          const tr_pool* pool, int32_t* q_start, int64_t rows, int64_t* slots,
+                          int32_t* pos, int32_t* short_of, void* stream);
+
+/* Verification of drafted tokens.  Rows are packed as in tr_step: sequence b's rows
+ * q_start[b] .. q_start[b + 1] - 1 are its last accepted token and its drafts (of which
+ * those past row width are given up, as if there were none).  Row i's probabilities target[i]
+ * (and draft[i], from which ids[i + 1] was drawn) are those of the token behind it.
+ *   The draft x = ids[i + 1] of row i is accepted while
+ *     accept[i] draft[i][x] < target[i][x];      draft NULL: drafts were certain, 1
+ *   accepted[b] = drafts accepted before the first that is not
+ *   A token t is drawn in the row r behind them: with weights max(target[r] -
+ *   draft[r], 0) where that row's draft was rejected, target[r] where all were
+ *   accepted (or those weights are all 0), t is the lowest token at which the sum of
+ *   weights up to it exceeds draw[b] times their sum; 0 where all are 0.
+ *   tokens[b]   = the accepted drafts, t, then -1                [seqs, width]
+ *   change[b]   = accepted[b] minus the sequence's drafts: what its length changes by
+ *                 (tr_update_pages)
+ * A sequence of no rows has tokens of -1 and 0s.  Probabilities need not be normed;
+ * NaN, negative and infinite ones count as 0.  accept and draw lie in [0, 1).  Drafts
+ * outside [0, vocab) are rejected.  Products, differences and sums are in 64 bits.
+ *   target, draft  device [T, vocab] of dtype, rows ld elements apart (>= vocab)
+ *   ids            device int32 [T]; accept device float [T]; draw device float [seqs]
+ *   scratch        device, tr_verify_scratch(seqs) bytes, 8-byte aligned, of one
+ *                  call at a time; its contents mean nothing before and after
+ * q_start is not checked by the host: rows outside [0, T) are never read. */
+size_t tr_verify_scratch(int32_t seqs);
+tr_status tr_verify_drafts(int64_t T, int32_t vocab, int32_t dtype, const void* target, int64_t ld_target,
+                           const void* draft, int64_t ld_draft, const int32_t* ids, int32_t seqs,
+                           const int32_t* q_start, const float* accept, const float* draw, int32_t width,
+                           int32_t* tokens, int32_t* accepted, int32_t* change, void* scratch, void* stream);
 
 /* Release the context and its scratch (NULL is a no-op).  Freeing device
  * memory waits for the device to finish outstanding work first. */

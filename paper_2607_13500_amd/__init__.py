@@ -9,7 +9,8 @@ Every step of the path runs in the HIP library libaltr.so (gfx950):
 * gather - byte copies of the kept rows into a compact [sum K, D] output.
 
 What a language model then does with the kept tokens (positions, rotated heads,
-a paged cache, attention over it) is in attention.py.
+a paged cache, attention over it) is in attention.py, what goes on around a step of it
+in step.py.
 
 This module only marshals torch tensors (device memory) and the current torch
 stream into the C ABI; it computes nothing itself.  If the library is missing
@@ -24,10 +25,12 @@ import torch
 
 from . import _lib
 from ._lib import Params
-from .attention import Attention, KVCache, Step, kept_positions
+from .attention import Attention, KVCache, KVCache8, Step, kept_positions
+from .step import PagePool, PageUpdate, Verified, update_pages, verify_drafts
 
 __all__ = ["Reducer", "ReduceResult", "TRError", "plan", "capacity_N", "reduce_noalloc", "LAMBDA_PAPER",
-           "Attention", "KVCache", "Step", "kept_positions"]
+           "Attention", "KVCache", "KVCache8", "Step", "kept_positions", "PagePool", "PageUpdate", "update_pages",
+           "Verified", "verify_drafts"]
 
 LAMBDA_PAPER = 1.0 / 3.0   # 64 importance + 128 diversity of 192 (efficiency setting)
 

@@ -67,6 +67,30 @@ class Cache(ctypes.Structure):
     ]
 
 
+class Cache8(ctypes.Structure):
+    """Mirror of tr_cache8 in include/tr.h."""
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("block", ctypes.c_int32),
+        ("page", ctypes.c_int64),
+        ("token", ctypes.c_int64),
+        ("head", ctypes.c_int64),
+        ("scale_page", ctypes.c_int64),
+        ("scale_block", ctypes.c_int64),
+        ("scale_head", ctypes.c_int64),
+    ]
+
+
+class Pool(ctypes.Structure):
+    """Mirror of tr_pool in include/tr.h."""
+    _fields_ = [("pages", ctypes.c_int32), ("ring", ctypes.c_void_p), ("state", ctypes.c_void_p), ("state_out", ctypes.c_void_p)]
+
+
 class StepArgs(ctypes.Structure):
     """Mirror of tr_step in include/tr.h."""
     _fields_ = [
@@ -151,6 +175,16 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.tr_append.restype = i32
     lib.tr_attend.argtypes = [vp, i64, H, P(Cache), P(StepArgs), ctypes.c_double, i32, i32, H, vp, vp]
     lib.tr_attend.restype = i32
+    lib.tr_append8.argtypes = [vp, i64, H, H, H, vp, vp, vp, i64, H, P(Cache8), P(StepArgs), vp]
+    lib.tr_append8.restype = i32
+    lib.tr_attend8.argtypes = [vp, i64, H, P(Cache8), P(StepArgs), ctypes.c_double, i32, i32, H, vp, vp]
+    lib.tr_attend8.restype = i32
+    lib.tr_update_pages.argtypes = [i32, vp, vp, vp, vp, i32, i64, i32, P(Pool), vp, i64, vp, vp, vp, vp]
+    lib.tr_update_pages.restype = i32
+    lib.tr_verify_scratch.argtypes = [i32]
+    lib.tr_verify_scratch.restype = ctypes.c_size_t
+    lib.tr_verify_drafts.argtypes = [i64, i32, i32, vp, i64, vp, i64, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    lib.tr_verify_drafts.restype = i32
     lib.tr_strerror.argtypes = [i32]
     lib.tr_strerror.restype = ctypes.c_char_p
     lib.tr_last_error.argtypes = []

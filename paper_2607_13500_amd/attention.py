@@ -8,6 +8,10 @@ between the reduction and the model's answer (the tr_attn calls of include/tr.h)
 * Attention.append        - the same on the way of new keys into a paged cache;
 * Attention.attend        - attention of the new tokens over that cache.
 
+append and attend take a cache of bf16 (or fp32) values, KVCache, or one of 8-bit
+values with a scale for each block of tokens and head, KVCache8.  What goes on around
+them in a step, its page tables and the verification of drafts, is in step.py.
+
 As elsewhere in the package this module only marshals torch tensors and the
 stream into the C ABI.
 """
@@ -17,12 +21,12 @@ import ctypes
 import math
 from array import array
 from itertools import chain
-from typing import NamedTuple, Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
 from . import _lib
-from ._lib import AttnParams, Cache, Heads, StepArgs
+from ._lib import AttnParams, Cache, Cache8, Heads, StepArgs
 
 # Small calls are bound by this module's own work (one decoded token: 9 us a call
 # against 12.5 us on the device), so each tensor is looked at once, devices are
@@ -57,6 +61,17 @@ class KVCache(NamedTuple):
     same) strides with the elements of a head side by side."""
     k: torch.Tensor
     v: torch.Tensor
+
+
+class KVCache8(NamedTuple):
+    """A paged cache in 8 bits: k and v float8_e4m3fn as in KVCache, and float32 scales
+    [pages, blocks, kv_heads] of any (the same) strides: row r of page g of head h
+    stands for k[g, r, h] * k_scale[g, r // (page_size // blocks), h].  append makes
+    the scales powers of two; attend takes any that are finite and >= 0."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
 
 
 class Step(NamedTuple):
@@ -244,18 +259,40 @@ class Attention:
             raise ValueError("%s must be a contiguous %s [%d] tensor on %s" % (name, self.dtype, self.head_dim, self.device))
         return w.data_ptr()
 
-    def _cache(self, cache: KVCache) -> Cache:
+    def _cache(self, cache):
+        if isinstance(cache, KVCache8):
+            return self._cache8(cache)
         k, v = cache
+        shape, stride = self._rows(k, v, self.dtype)
+        return Cache(k.data_ptr(), v.data_ptr(), shape[0], shape[1], stride[0], stride[1], stride[2])
+
+    def _cache8(self, cache: KVCache8) -> Cache8:
+        k, v, k_scale, v_scale = cache
+        shape, stride = self._rows(k, v, torch.float8_e4m3fn)
+        for name, t in (("cache.k_scale", k_scale), ("cache.v_scale", v_scale)):
+            if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype is not torch.float32:
+                raise ValueError("%s must be a float32 tensor on %s" % (name, self.device))
+        scales, step = k_scale.shape, k_scale.stride()
+        if len(scales) != 3 or scales[0] != shape[0] or scales[2] != self.kv_heads or not scales[1] or shape[1] % scales[1]:
+            raise ValueError("cache.k_scale must be [%d, blocks, %d] with blocks that divide page_size %d, got %s"
+                             % (shape[0], self.kv_heads, shape[1], tuple(scales)))
+        if scales != v_scale.shape or step != v_scale.stride():
+            raise ValueError("cache.k_scale and cache.v_scale must have the same shape and strides")
+        return Cache8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0], shape[1], shape[1] // scales[1],
+                      stride[0], stride[1], stride[2], step[0], step[1], step[2])
+
+    def _rows(self, k, v, dtype):
+        """Shape and strides of a cache's keys and values."""
         for name, t in (("cache.k", k), ("cache.v", v)):
-            if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype is not self.dtype:
-                raise ValueError("%s must be a %s tensor on %s" % (name, self.dtype, self.device))
+            if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype is not dtype:
+                raise ValueError("%s must be a %s tensor on %s" % (name, dtype, self.device))
         shape, stride = k.shape, k.stride()
         if len(shape) != 4 or shape[2] != self.kv_heads or shape[3] != self.head_dim or (self.head_dim > 1 and stride[3] != 1):
             raise ValueError("cache.k must be [pages, page_size, %d, %d] with unit element stride, got %s of strides %s"
                              % (self.kv_heads, self.head_dim, tuple(shape), stride))
         if shape != v.shape or stride != v.stride():
             raise ValueError("cache.k and cache.v must have the same shape and strides")
-        return Cache(k.data_ptr(), v.data_ptr(), shape[0], shape[1], stride[0], stride[1], stride[2])
+        return shape, stride
 
     def _step(self, step: Step) -> StepArgs:
         for name, t in zip(Step._fields, step):
@@ -332,13 +369,18 @@ class Attention:
                                            self._stream(stream)), "tr_rotate_backward")
         return outs[0], outs[1], dw[0], dw[1]
 
-    def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, cache: KVCache,
-               step: Step, *, wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
+    def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
+               cache: Union[KVCache, KVCache8], step: Step, *, wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
                q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
         """rotate for the new tokens of a step: their keys go to their place in
         the cache, their values (as they are) beside them; returns q_out (None
         where q is).  Slices of one projection's output are fine.  Passes no
-        gradient."""
+        gradient.
+
+        Into a KVCache8 keys and values are rounded to e4m3 once, each block and head
+        with the smallest power of two as its scale that its largest new element asks
+        for; in a block that holds older tokens of the sequence the scale grows only if
+        it has to, and they are rounded again.  What is not finite becomes NaN."""
         tokens = k.shape[0]
         hk, hv = self._heads("k", k, self.kv_heads, tokens), self._heads("v", v, self.kv_heads, tokens)
         hq = oq = _NONE
@@ -346,16 +388,18 @@ class Attention:
             hq = self._heads("q", q, self.heads, tokens)
             q_out, oq = self._out("q_out", q_out, tokens, self.heads, stream)
         at, ldpos = self._pos(pos, tokens)
-        status = self.lib.tr_append(self._ctx, tokens, hq, hk, hv, self._weight("wq", wq), self._weight("wk", wk), at,
+        call = self.lib.tr_append8 if isinstance(cache, KVCache8) else self.lib.tr_append
+        status = call(self._ctx, tokens, hq, hk, hv, self._weight("wq", wq), self._weight("wk", wk), at,
                                     ldpos, oq, self._cache(cache), self._step(step), self._stream(stream))
-        _check(status, "tr_append")
+        _check(status, call.__name__)
         return q_out if q is not None else None
 
-    def attend(self, q: torch.Tensor, cache: KVCache, step: Step, *, scale: Optional[float] = None,
+    def attend(self, q: torch.Tensor, cache: Union[KVCache, KVCache8], step: Step, *, scale: Optional[float] = None,
                causal: bool = True, window: int = 0, out: Optional[torch.Tensor] = None, want_lse: bool = False,
                stream=None):
         """(out, lse): attention of the new tokens' queries q [tokens, heads,
-        head_dim] over their sequences' tokens in the cache (bf16).
+        head_dim] over their sequences' tokens in the cache (bf16; a KVCache8's
+        keys and values are widened to bf16 without loss, head_dim a multiple of 16).
 
         causal: a token sees itself and those before it, with window > 0 the last
         `window` of them; otherwise all kv_len tokens of its sequence.  A row
@@ -367,10 +411,11 @@ class Attention:
         hq = self._heads("q", q, self.heads, tokens)
         out, ho = self._out("out", out, tokens, self.heads, stream)
         lse = _empty((tokens, self.heads), torch.float32, self.device, stream) if want_lse else None
-        status = self.lib.tr_attend(self._ctx, tokens, hq, self._cache(cache), self._step(step),
+        call = self.lib.tr_attend8 if isinstance(cache, KVCache8) else self.lib.tr_attend
+        status = call(self._ctx, tokens, hq, self._cache(cache), self._step(step),
                                     1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), 1 if causal else 0,
                                     int(window), ho, _ptr(lse), self._stream(stream))
-        _check(status, "tr_attend")
+        _check(status, call.__name__)
         return out, lse
 
     def close(self):

@@ -57,6 +57,15 @@ struct RotateArgs {
     tr_step step;
 };
 
+// An append call on a cache of 8-bit values.  `cache` has no memory: its pages and rows
+// say which queries belong to a sequence.
+struct Append8Args : RotateArgs {
+    tr_cache8 cache8;
+    int64_t candidates;        // of segments; filled in by the launch
+};
+
+hipError_t launch_append8(const Append8Args& a, bool bf16, hipStream_t s);
+
 // Floats of RotateArgs::part for head_dim dim on a device of cus compute units.
 size_t rotate_part_floats(int dim, int cus);
 hipError_t launch_rotate(const RotateArgs& a, bool bf16, hipStream_t s);
@@ -87,10 +96,18 @@ struct AttendArgs {
     int32_t cus;
 };
 
+// Over a cache of 8-bit values.  `cache` has no memory: its pages and their size say
+// where tokens lie.
+struct Attend8Args : AttendArgs {
+    tr_cache8 cache8;
+    Divisor by_block;
+};
+
 // group, the divisors, most, scale, keep and flip are filled in by the launch.
 size_t attend_part_floats(int dim, int cus);
 size_t attend_groups(int cus);
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend8(const Attend8Args& a, hipStream_t s);
 
 // ---- device helpers ------------------------------------------------------------
 // A value that is the same in all lanes, as a scalar.

@@ -128,6 +128,19 @@ tr_status check_tokens(const tr_attn* a, int64_t T)
     return TR_OK;
 }
 
+tr_status check_step(const tr_step* s)
+{
+    if (s->seqs < 1) return fail(TR_EINVAL, "seqs must be >= 1 where there are tokens (got %d)", s->seqs);
+    if (s->table_width < 0 || s->table_stride < 0)
+        return fail(TR_EINVAL, "table_width = %d and table_stride = %lld must be >= 0", s->table_width,
+                    (long long)s->table_stride);
+    if (!s->q_start || !s->kv_len || (!s->table && s->table_width))
+        return fail(TR_EINVAL, "q_start, kv_len and table must be non-NULL");
+    if (((uintptr_t)s->q_start | (uintptr_t)s->kv_len | (uintptr_t)s->table) & 3u)
+        return fail(TR_EUNSUPPORTED, "q_start, kv_len and table must be 4-byte aligned");
+    return TR_OK;
+}
+
 tr_status check_cache(const tr_attn* a, const tr_cache* c, const tr_step* s)
 {
     if (!c || !s) return fail(TR_EINVAL, "cache and step must be non-NULL");
@@ -140,15 +153,37 @@ tr_status check_cache(const tr_attn* a, const tr_cache* c, const tr_step* s)
     if (rows_overlap({{c->page, c->pages}, {c->token, c->page_size}, {c->head, a->p.kv_heads}}, dim))
         return fail(TR_EINVAL, "the cache has rows that overlap (strides %lld, %lld and %lld, rows of %lld elements)",
                     (long long)c->page, (long long)c->token, (long long)c->head, (long long)dim);
-    if (s->seqs < 1) return fail(TR_EINVAL, "seqs must be >= 1 where there are tokens (got %d)", s->seqs);
-    if (s->table_width < 0 || s->table_stride < 0)
-        return fail(TR_EINVAL, "table_width = %d and table_stride = %lld must be >= 0", s->table_width,
-                    (long long)s->table_stride);
-    if (!s->q_start || !s->kv_len || (!s->table && s->table_width))
-        return fail(TR_EINVAL, "q_start, kv_len and table must be non-NULL");
-    if (((uintptr_t)s->q_start | (uintptr_t)s->kv_len | (uintptr_t)s->table) & 3u)
-        return fail(TR_EUNSUPPORTED, "q_start, kv_len and table must be 4-byte aligned");
-    return TR_OK;
+    return check_step(s);
+}
+
+// The same for a cache of 8-bit values.
+tr_status check_cache8(const tr_attn* a, const tr_cache8* c, const tr_step* s)
+{
+    if (!c || !s) return fail(TR_EINVAL, "cache and step must be non-NULL");
+    if (c->pages < 1 || c->page_size < 1 || c->block < 1 || c->page_size % c->block)
+        return fail(TR_EINVAL, "the cache needs pages >= 1, page_size >= 1 and a block that divides it (got %d, %d and %d)", c->pages,
+                    c->page_size, c->block);
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale)
+        return fail(TR_EINVAL, "the cache's k, v, k_scale and v_scale must be non-NULL");
+    if (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 3u)
+        return fail(TR_EUNSUPPORTED, "k_scale and v_scale must be 4-byte aligned");
+    const int64_t dim = a->p.head_dim;
+    if (rows_overlap({{c->page, c->pages}, {c->token, c->page_size}, {c->head, a->p.kv_heads}}, dim))
+        return fail(TR_EINVAL, "the cache has rows that overlap (strides %lld, %lld and %lld, rows of %lld elements)",
+                    (long long)c->page, (long long)c->token, (long long)c->head, (long long)dim);
+    if (rows_overlap({{c->scale_page, c->pages}, {c->scale_block, c->page_size / c->block}, {c->scale_head, a->p.kv_heads}}, 1))
+        return fail(TR_EINVAL, "the cache has scales that overlap (strides %lld, %lld and %lld)", (long long)c->scale_page,
+                    (long long)c->scale_block, (long long)c->scale_head);
+    return check_step(s);
+}
+
+// Its pages and rows without memory, as the code for any cache looks at them.
+tr_cache pages_of(const tr_cache8* c)
+{
+    tr_cache r{};
+    r.pages = c->pages;
+    r.page_size = c->page_size;
+    return r;
 }
 
 // The fields that every call on heads shares.
@@ -171,6 +206,81 @@ tr::RotateArgs rotate_args(const tr_attn* a, int64_t T, const void* wq, const vo
     r.part = a->part;
     r.cus = a->cus;
     return r;
+}
+
+// What an append call has besides its cache and step.
+tr_status check_append(const tr_attn* a, int64_t T, const tr_heads& q, const tr_heads& k, const tr_heads& v, const void* wq,
+                       const void* wk, const int32_t* pos, int64_t ldpos, const tr_heads& q_out)
+{
+    tr_status st;
+    if ((st = check_heads("k", k, a->eb, T, a->p.kv_heads)) != TR_OK || (st = check_heads("v", v, a->eb, T, a->p.kv_heads)) != TR_OK)
+        return st;
+    if (q.p && ((st = check_heads("q", q, a->eb, T, a->p.heads)) != TR_OK ||
+                (st = check_out_heads("q_out", q_out, a->eb, T, a->p.heads, a->p.head_dim)) != TR_OK))
+        return st;
+    if ((st = check_weights(a, wq, wk)) != TR_OK) return st;
+    return check_positions(a, pos, ldpos);
+}
+
+tr::RotateArgs append_args(const tr_attn* a, int64_t T, const tr_heads& q, const tr_heads& k, const tr_heads& v, const void* wq,
+                           const void* wk, const int32_t* pos, int64_t ldpos, const tr_heads& q_out, const tr_step* s)
+{
+    tr::RotateArgs r = rotate_args(a, T, wq, wk, pos, ldpos);
+    r.heads[0] = q.p ? a->p.heads : 0;
+    r.heads[1] = r.heads[2] = a->p.kv_heads;
+    r.in[0] = q;
+    r.in[1] = k;
+    r.in[2] = v;
+    r.out[0] = q_out;
+    r.append = true;
+    r.step = *s;
+    return r;
+}
+
+// What an attend call asks of a context and of its numbers.
+tr_status check_attend(const tr_attn* a, int64_t T, int multiple, double scale, int32_t causal, int32_t window)
+{
+    tr_status st = check_tokens(a, T);
+    if (st != TR_OK) return st;
+    if (a->p.dtype != TR_BF16) return fail(TR_EUNSUPPORTED, "attention needs a bf16 context");
+    if (a->p.head_dim % multiple) return fail(TR_EUNSUPPORTED, "attention needs head_dim %% %d == 0 (got %d)", multiple, a->p.head_dim);
+    if (!isfinite((float)scale)) return fail(TR_EINVAL, "scale must be finite in fp32 (got %g)", scale);
+    if (causal != 0 && causal != 1) return fail(TR_EINVAL, "causal must be 0 or 1 (got %d)", causal);
+    if (window < 0 || (window > 0 && !causal))
+        return fail(TR_EINVAL, "window must be >= 0, and 0 without causal (got %d)", window);
+    return TR_OK;
+}
+
+// Its queries and outputs.  `cache`: whether the cache's bases and strides are of 16 bytes.
+tr_status check_rows(const tr_attn* a, int64_t T, const tr_heads& q, const tr_heads& out, const float* lse, bool cache)
+{
+    tr_status st;
+    if ((st = check_heads("q", q, a->eb, T, a->p.heads)) != TR_OK ||
+        (st = check_out_heads("out", out, a->eb, T, a->p.heads, a->p.head_dim)) != TR_OK)
+        return st;
+    if (!aligned16(q.p) || !aligned16(out.p) || (q.token | q.head | out.token | out.head) % 8 || !cache)
+        return fail(TR_EUNSUPPORTED, "q, out and the cache need bases and strides of 16 bytes");
+    if ((uintptr_t)lse & 3u) return fail(TR_EUNSUPPORTED, "lse must be 4-byte aligned");
+    return TR_OK;
+}
+
+void fill_attend(tr::AttendArgs& r, const tr_attn* a, int64_t T, const tr_heads& q, const tr_step* s, double scale, int32_t causal,
+                 int32_t window, const tr_heads& out, float* lse)
+{
+    r.tokens = T;
+    r.heads = a->p.heads;
+    r.kv_heads = a->p.kv_heads;
+    r.dim = a->p.head_dim;
+    r.q = q;
+    r.out = out;
+    r.step = *s;
+    r.raw_scale = (float)scale;
+    r.causal = causal;
+    r.window = window;
+    r.lse = lse;
+    r.part = a->parts;
+    r.arrived = a->arrived;
+    r.cus = a->cus;
 }
 
 }  // namespace
@@ -374,27 +484,31 @@ tr_status tr_append(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, c
     Range range("tr_append");
     tr_status st = check_tokens(a, T);
     if (st != TR_OK || T == 0) return st;
-    const int dim = a->p.head_dim;
-    if ((st = check_cache(a, c, s)) != TR_OK || (st = check_heads("k", k, a->eb, T, a->p.kv_heads)) != TR_OK ||
-        (st = check_heads("v", v, a->eb, T, a->p.kv_heads)) != TR_OK)
-        return st;
-    if (q.p && ((st = check_heads("q", q, a->eb, T, a->p.heads)) != TR_OK ||
-                (st = check_out_heads("q_out", q_out, a->eb, T, a->p.heads, dim)) != TR_OK))
-        return st;
-    if ((st = check_weights(a, wq, wk)) != TR_OK || (st = check_positions(a, pos, ldpos)) != TR_OK) return st;
+    if ((st = check_cache(a, c, s)) != TR_OK || (st = check_append(a, T, q, k, v, wq, wk, pos, ldpos, q_out)) != TR_OK) return st;
     DeviceGuard g(a->device);
     if (!g.ok) return fail(TR_EDEVICE, "hipSetDevice(%d) failed", a->device);
-    tr::RotateArgs r = rotate_args(a, T, wq, wk, pos, ldpos);
-    r.heads[0] = q.p ? a->p.heads : 0;
-    r.heads[1] = r.heads[2] = a->p.kv_heads;
-    r.in[0] = q;
-    r.in[1] = k;
-    r.in[2] = v;
-    r.out[0] = q_out;
-    r.append = true;
+    tr::RotateArgs r = append_args(a, T, q, k, v, wq, wk, pos, ldpos, q_out, s);
     r.cache = *c;
-    r.step = *s;
     hipError_t e = tr::launch_rotate(r, a->p.dtype == TR_BF16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "append kernel launch");
+    return TR_OK;
+}
+
+tr_status tr_append8(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, const void* wq, const void* wk,
+                     const int32_t* pos, int64_t ldpos, tr_heads q_out, const tr_cache8* c, const tr_step* s, void* stream)
+{
+    clear_error();
+    Range range("tr_append8");
+    tr_status st = check_tokens(a, T);
+    if (st != TR_OK || T == 0) return st;
+    if ((st = check_cache8(a, c, s)) != TR_OK || (st = check_append(a, T, q, k, v, wq, wk, pos, ldpos, q_out)) != TR_OK) return st;
+    DeviceGuard g(a->device);
+    if (!g.ok) return fail(TR_EDEVICE, "hipSetDevice(%d) failed", a->device);
+    tr::Append8Args r{};
+    static_cast<tr::RotateArgs&>(r) = append_args(a, T, q, k, v, wq, wk, pos, ldpos, q_out, s);
+    r.cache = pages_of(c);
+    r.cache8 = *c;
+    hipError_t e = tr::launch_append8(r, a->p.dtype == TR_BF16, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "append kernel launch");
     return TR_OK;
 }
@@ -404,42 +518,38 @@ tr_status tr_attend(tr_attn* a, int64_t T, tr_heads q, const tr_cache* c, const 
 {
     clear_error();
     Range range("tr_attend");
-    tr_status st = check_tokens(a, T);
-    if (st != TR_OK) return st;
-    if (a->p.dtype != TR_BF16) return fail(TR_EUNSUPPORTED, "tr_attend needs a bf16 context");
-    if (a->p.head_dim % 8) return fail(TR_EUNSUPPORTED, "tr_attend needs head_dim %% 8 == 0 (got %d)", a->p.head_dim);
-    if (!isfinite((float)scale)) return fail(TR_EINVAL, "scale must be finite in fp32 (got %g)", scale);
-    if (causal != 0 && causal != 1) return fail(TR_EINVAL, "causal must be 0 or 1 (got %d)", causal);
-    if (window < 0 || (window > 0 && !causal))
-        return fail(TR_EINVAL, "window must be >= 0, and 0 without causal (got %d)", window);
-    if (T == 0) return TR_OK;
-    const int dim = a->p.head_dim;
-    if ((st = check_cache(a, c, s)) != TR_OK || (st = check_heads("q", q, a->eb, T, a->p.heads)) != TR_OK ||
-        (st = check_out_heads("out", out, a->eb, T, a->p.heads, dim)) != TR_OK)
+    tr_status st = check_attend(a, T, 8, scale, causal, window);
+    if (st != TR_OK || T == 0) return st;
+    if ((st = check_cache(a, c, s)) != TR_OK ||
+        (st = check_rows(a, T, q, out, lse, aligned16(c->k) && aligned16(c->v) && (c->page | c->token | c->head) % 8 == 0)) != TR_OK)
         return st;
-    if (!aligned16(q.p) || !aligned16(out.p) || !aligned16(c->k) || !aligned16(c->v) ||
-        (q.token | q.head | out.token | out.head | c->page | c->token | c->head) % 8)
-        return fail(TR_EUNSUPPORTED, "q, out and the cache need bases and strides of 16 bytes");
-    if ((uintptr_t)lse & 3u) return fail(TR_EUNSUPPORTED, "lse must be 4-byte aligned");
     DeviceGuard g(a->device);
     if (!g.ok) return fail(TR_EDEVICE, "hipSetDevice(%d) failed", a->device);
     tr::AttendArgs r{};
-    r.tokens = T;
-    r.heads = a->p.heads;
-    r.kv_heads = a->p.kv_heads;
-    r.dim = dim;
-    r.q = q;
-    r.out = out;
+    fill_attend(r, a, T, q, s, scale, causal, window, out, lse);
     r.cache = *c;
-    r.step = *s;
-    r.raw_scale = (float)scale;
-    r.causal = causal;
-    r.window = window;
-    r.lse = lse;
-    r.part = a->parts;
-    r.arrived = a->arrived;
-    r.cus = a->cus;
     hipError_t e = tr::launch_attend(r, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
+    return TR_OK;
+}
+
+tr_status tr_attend8(tr_attn* a, int64_t T, tr_heads q, const tr_cache8* c, const tr_step* s, double scale, int32_t causal,
+                     int32_t window, tr_heads out, float* lse, void* stream)
+{
+    clear_error();
+    Range range("tr_attend8");
+    tr_status st = check_attend(a, T, 16, scale, causal, window);
+    if (st != TR_OK || T == 0) return st;
+    if ((st = check_cache8(a, c, s)) != TR_OK ||
+        (st = check_rows(a, T, q, out, lse, aligned16(c->k) && aligned16(c->v) && (c->page | c->token | c->head) % 16 == 0)) != TR_OK)
+        return st;
+    DeviceGuard g(a->device);
+    if (!g.ok) return fail(TR_EDEVICE, "hipSetDevice(%d) failed", a->device);
+    tr::Attend8Args r{};
+    fill_attend(r, a, T, q, s, scale, causal, window, out, lse);
+    r.cache = pages_of(c);
+    r.cache8 = *c;
+    hipError_t e = tr::launch_attend8(r, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
     return TR_OK;
 }

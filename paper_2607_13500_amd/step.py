@@ -1,0 +1,144 @@
+"""What goes on around the attention of a step (tr_update_pages and tr_verify_drafts of
+include/tr.h):
+
+* update_pages   - page tables, row starts, slots and positions from the sequences'
+                   lengths and what they gain or lose;
+* verify_drafts  - how many drafted tokens the target's probabilities accept, and the
+                   token drawn behind them, from given random numbers.
+
+A decoding step with drafts is update_pages, the model (Attention.append and attend
+in each layer), verify_drafts, and its `change` goes into the next update_pages.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import _lib
+from ._lib import Pool
+from .attention import _DTYPES, Step, _check, _empty, _raw_stream
+
+
+class PagePool(NamedTuple):
+    """Free pages of a cache: a ring int32 [pages] of page numbers, state[1] of them
+    from index state[0] on.  A new cache's: arange(pages) and [0, pages]."""
+    ring: torch.Tensor
+    state: torch.Tensor            # int32 [2]
+
+
+class PageUpdate(NamedTuple):
+    step: Step                     # q_start, the new lengths, the table
+    slots: torch.Tensor            # int64 [rows] page * page_size + row of each new token, -1 behind them
+    pos: torch.Tensor              # int32 [rows] its place in its sequence, 0 behind them
+    pool: PagePool                 # the ring and its new state
+    short: torch.Tensor            # int32 [1]: 0, or the pages that are lacking (then nothing has changed)
+
+
+class Verified(NamedTuple):
+    tokens: torch.Tensor           # int32 [seqs, width]: accepted drafts, the drawn token, then -1
+    accepted: torch.Tensor         # int32 [seqs] accepted drafts
+    change: torch.Tensor           # int32 [seqs] accepted minus drafted: what the sequence's length changes by
+
+
+def _vector(name, t, device, dtype, size):
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype is not dtype or t.shape != (size,) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s [%d] tensor on %s" % (name, dtype, size, device))
+    return t.data_ptr()
+
+
+def _run(call, name, index, stream, *args):
+    handle = _raw_stream(index) if stream is None else stream.cuda_stream
+    if index == torch.cuda.current_device():
+        status = call(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            status = call(*args, handle)
+    _check(status, name)
+
+
+def update_pages(change: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor, pool: PagePool, page_size: int, rows: int, *,
+                 in_place: bool = False, stream=None) -> PageUpdate:
+    """The next step of sequences of kv_len tokens: sequence b gains change[b] new
+    tokens, or loses its last -change[b] (all, if it has fewer).
+
+    Each holds ceil(length / page_size) pages in its row of `table`, which is updated
+    in place as the pool's ring is: pages are taken from the ring's front, and those of
+    lost tokens go to its end, where the same call does not take them.  `rows` is the
+    room for new tokens' slots and positions (packed as step.q_start says).  If the
+    pool lacks pages, a sequence outgrows its row of the table or the new tokens the
+    rows, nothing changes, no row belongs to any sequence, and `short` is the number of
+    lacking pages, in the last two cases 2^31 - 1.
+
+    in_place: the new lengths and the pool's new state are written to kv_len and
+    pool.state themselves, as a recorded graph that is replayed needs it.
+    """
+    if not isinstance(kv_len, torch.Tensor) or not kv_len.is_cuda or kv_len.dim() != 1:
+        raise ValueError("kv_len must be an int32 [seqs] tensor on a ROCm device")
+    device, seqs = kv_len.device, kv_len.shape[0]
+    i32 = torch.int32
+    _vector("kv_len", kv_len, device, i32, seqs)
+    if not isinstance(table, torch.Tensor) or table.device != device or table.dtype is not i32 or table.dim() != 2 \
+            or table.shape[0] != seqs or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be an int32 [%d, width] tensor with rows contiguous on %s" % (seqs, device))
+    ring, state = pool
+    if not isinstance(ring, torch.Tensor) or ring.dim() != 1:
+        raise ValueError("pool.ring must be an int32 [pages] tensor on %s" % device)
+    rows = int(rows)
+    if rows < 0:
+        raise ValueError("rows must be >= 0 (got %d)" % rows)
+    sizes = [seqs + 1, rows, 1] if in_place else [seqs + 1, rows, 1, seqs, 2]
+    parts = _empty((sum(sizes),), i32, device, stream).split(sizes)
+    q_start, pos, short = parts[:3]
+    kv_out, state_out = (kv_len, state) if in_place else parts[3:]
+    slots = _empty((rows,), torch.int64, device, stream)
+    p = Pool(ring.shape[0], _vector("pool.ring", ring, device, i32, ring.shape[0]), _vector("pool.state", state, device, i32, 2),
+             state_out.data_ptr())
+    _run(_lib.load().tr_update_pages, "tr_update_pages", device.index, stream, seqs, _vector("change", change, device, i32, seqs),
+         kv_len.data_ptr(), kv_out.data_ptr(), table.data_ptr(), table.shape[1], table.stride(0), int(page_size), ctypes.byref(p),
+         q_start.data_ptr(), rows, slots.data_ptr(), pos.data_ptr(), short.data_ptr())
+    return PageUpdate(Step(q_start, kv_out, table), slots, pos, PagePool(ring, state_out), short)
+
+
+def _rows(name, t, device, dtype, shape):
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype is not dtype or t.shape != shape \
+            or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a %s %s tensor with rows contiguous on %s" % (name, dtype, list(shape), device))
+    return t.data_ptr(), t.stride(0)
+
+
+def verify_drafts(target: torch.Tensor, ids: torch.Tensor, q_start: torch.Tensor, accept: torch.Tensor, draw: torch.Tensor,
+                  width: int, *, draft: Optional[torch.Tensor] = None, stream=None) -> Verified:
+    """Drafted tokens against the target's probabilities.
+
+    Rows are packed as in a Step: sequence b's rows q_start[b] .. q_start[b + 1] - 1 are
+    its last accepted token and its drafts, ids int32 [tokens].  Row i of target
+    (float32 or bfloat16 [tokens, vocab]) is the distribution of the token behind it,
+    that of draft the one from which ids[i + 1] was drawn (None: drafts were certain).
+
+    A draft x of row i is accepted while accept[i] * draft[i, x] < target[i, x].
+    Behind the accepted ones a token is drawn with draw[b]: from max(target - draft, 0)
+    of the first rejected draft's row, from the last row's target where all were
+    accepted; it is the lowest token at which the weights' sum exceeds draw[b] times
+    the whole.  At most width - 1 drafts of a sequence are looked at.  accept (float32
+    [tokens]) and draw (float32 [seqs]) lie in [0, 1).  Exact in 64 bits for the given
+    numbers: the same ones give the same tokens.
+    """
+    if not isinstance(target, torch.Tensor) or not target.is_cuda or target.dim() != 2 or target.dtype not in _DTYPES:
+        raise ValueError("target must be a float32 or bfloat16 [tokens, vocab] tensor on a ROCm device")
+    if not isinstance(q_start, torch.Tensor) or q_start.dim() != 1 or q_start.shape[0] < 1:
+        raise ValueError("q_start must be an int32 [seqs + 1] tensor on %s" % target.device)
+    device, (tokens, vocab), seqs, width, i32 = target.device, target.shape, q_start.shape[0] - 1, int(width), torch.int32
+    if width < 1:
+        raise ValueError("width must be >= 1 (got %d)" % width)
+    p, ld = _rows("target", target, device, target.dtype, target.shape)
+    q, ld_draft = (None, 0) if draft is None else _rows("draft", draft, device, target.dtype, target.shape)
+    lib = _lib.load()
+    said, accepted, change = _empty((seqs * (width + 2),), i32, device, stream).split([seqs * width, seqs, seqs])
+    scratch = _empty((lib.tr_verify_scratch(seqs),), torch.uint8, device, stream)
+    _run(lib.tr_verify_drafts, "tr_verify_drafts", device.index, stream, tokens, vocab, _DTYPES[target.dtype], p, ld, q, ld_draft,
+         _vector("ids", ids, device, i32, tokens), seqs, _vector("q_start", q_start, device, i32, seqs + 1),
+         _vector("accept", accept, device, torch.float32, tokens), _vector("draw", draw, device, torch.float32, seqs), width,
+         said.data_ptr(), accepted.data_ptr(), change.data_ptr(), scratch.data_ptr())
+    return Verified(said.view(seqs, width), accepted, change)
