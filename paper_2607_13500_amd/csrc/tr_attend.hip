@@ -377,15 +377,6 @@ __global__ __launch_bounds__(kFewThreads, kFewPerCu<DH>) void attend_few_kernel(
 // at piece c ^ f(r), which the loads bring about by each lane's choice of source
 // (they fill shared memory in lane order).  f spreads the rows that one read of
 // 16 (keys) or 4 (values) rows touches over all banks.
-constexpr int kManyTile = 64, kManyRows = 32;
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-template <int DH>
-__device__ __forceinline__ int v_swizzle(int row)
-{
-    return DH == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
-}
 
 // PG16: pages of whole 16 tokens, below 2 GB: the rows that one wavefront's load
 // fills lie in one page, whose address is the wavefront's.

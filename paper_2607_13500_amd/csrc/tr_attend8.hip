@@ -9,6 +9,7 @@
 // key's multiplies its scores, together with the softmax's scale, and a value's its
 // weights, in fp32, before these are rounded to bf16.
 #include <algorithm>
+#include <type_traits>
 
 #include "tr_attend_work.h"
 
@@ -19,17 +20,19 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
-// Eight e4m3 values as bf16.
-__device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b)
+__device__ __forceinline__ float lane_of(float x, int i) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), i)); }
+
+// Eight e4m3 values as bf16, times a power of two.
+__device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float by = 1.f)
 {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     struct {
         bf16x2 v[4];
     } r;
-    r.v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false);
-    r.v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
-    r.v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false);
-    r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+    r.v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, false);
+    r.v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, true);
+    r.v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, false);
+    r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, true);
     return __builtin_bit_cast(bf16x8, r);
 }
 
@@ -400,6 +403,426 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
     }
 }
 
+// ---- many rows ---------------------------------------------------------------------------
+// A workgroup of NW wavefronts of 32 rows each over the same keys, in tiles of 64 that
+// are widened on their way into shared memory, two tiles there at a time: of the next
+// one the bytes are in registers, of the one after it on their way there.  Widening in
+// the stage is shared by all wavefronts; from there on a tile is the bf16 kernel's, whose
+// bounds (matrix instructions and the softmax between them) are this one's.
+//
+// Values' scales that are powers of two go into the widening, which is exact, else
+// they multiply the weights.  Keys' scales multiply scores, in the multiply-add that
+// takes the maximum off.
+// Whether a scale is a power of two (and a normal number) by which widening is exact.
+__device__ __forceinline__ bool is_power(float s)
+{
+    const uint32_t w = __float_as_uint(s);
+    return (w & 0x807fffffu) == 0 && w - (10u << 23) < (238u << 23);       // 2^-117 .. 2^120
+}
+
+// UNI: pages and blocks of whole 16 tokens, so that a scale is that of 16 keys.
+template <int DH, int NW, int STEP, bool UNI, bool FULL>
+__global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kernel(Attend8Args a)
+{
+    constexpr int ROWS = NW * kManyRows, T = NW * 64;
+    constexpr int KF = DH / 16, DT = DH / 32;               // fragments of keys, tiles of elements
+    constexpr int BYTES = kManyTile * DH * 2;               // of a widened tile
+    constexpr int PIECES = DH / 16, NP = kManyTile * PIECES;   // pieces of a row and of a tile, 16 bytes each
+    constexpr int NI = 2 * NP / T;                          // of a thread, keys' before values'
+    __shared__ __align__(16) unsigned char smem[4 * BYTES]; // stage 0: K, V; stage 1: K, V
+    __shared__ int flag;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+
+    const Shares all = shares_of<ROWS, STEP>(a, lane);
+    const bool by_item = STEP == 0 || items_alone<ROWS, STEP>(a, all, lane);
+    int64_t u, u_end = 0;
+    if (by_item) {
+        // whole items, the last ones (which see most) first
+        u = (STEP == 0 ? all.total : shares_of<ROWS, 0>(a, lane).total) - 1 - (int64_t)blockIdx.x;
+        if (u < 0) return;
+    } else {
+        u = (int64_t)blockIdx.x * all.share;
+        u_end = min(u + all.share, all.total);
+    }
+    int from = 0;
+    int64_t before = 0;
+    while (by_item ? u >= 0 : u < u_end) {
+        const Place pl = by_item ? place_of<ROWS, 0>(a, u, lane) : place_of<ROWS, STEP>(a, u, lane, from, before);
+        from = pl.b;
+        before = pl.first;
+        const Sequence s = pl.s;
+        const int64_t local = u - pl.first;
+        const int item = (int)(local / pl.steps), step0 = (int)(local - (int64_t)item * pl.steps);
+        const int step1 = by_item ? 1 : (int)min((int64_t)pl.steps, step0 + (u_end - u));
+        const int rt = item / a.kv_heads, h = item - rt * a.kv_heads;
+        const bool whole = by_item || (step0 == 0 && step1 == pl.steps);
+
+        // ---- rows: this lane's, the wavefront's and the workgroup's -------------------
+        const int rows = (int)min((int64_t)ROWS, (int64_t)s.n * a.group - (int64_t)rt * ROWS);
+        const int wrow = wave * kManyRows, my = wrow + col;
+        const bool live = my < rows;
+        const uint32_t r = (uint32_t)rt * ROWS + my;
+        const int tok = (int)divide(r, a.by_group), head = h * a.group + (int)(r - (uint32_t)tok * a.group);
+        int lo = 0, hi = 0;
+        if (live) seen_by(a, s, tok, lo, hi);
+        auto bounds = [&](int r0, int r1, int& lo0, int& hi0, int& lo1, int& hi1) {    // of rows r0 .. r1 of the tile
+            seen_by(a, s, (int)divide((uint32_t)rt * ROWS + r0, a.by_group), lo0, hi0);
+            seen_by(a, s, (int)divide((uint32_t)rt * ROWS + r1, a.by_group), lo1, hi1);
+        };
+        int lo_min, hi_min, lo_max, hi_max, wlo_min = 0, whi_min = 0, wlo_max = 0, whi_max = 0;
+        bounds(0, rows - 1, lo_min, hi_min, lo_max, hi_max);
+        const bool works = wrow < rows;
+        if (works) bounds(wrow, min(rows, wrow + kManyRows) - 1, wlo_min, whi_min, wlo_max, whi_max);
+        const bool full_rows = wrow + kManyRows <= rows;
+
+        bf16x8 qf[KF];
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+            u32x4 v{};
+            if (live && (FULL || k * 16 + half * 8 < a.dim))
+                v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q.p) + (s.q0 + tok) * a.q.token + (int64_t)head * a.q.head + k * 16 + half * 8);
+            // scale < 0: that of -q; scale 0: scores of q = 0, NaN where it is not finite
+            if (a.keep == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[i] = ((v[i] & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u);
+            }
+            v ^= a.flip;
+            qf[k] = __builtin_bit_cast(bf16x8, v);
+        }
+        f32x16 o[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
+        float m = minus_inf(), l = 0.f;           // m: of the scores in powers of two
+
+        // ---- keys ---------------------------------------------------------------------
+        const int base = s.begin & ~(kAlign - 1);
+        int j0 = base + step0 * STEP;
+        if (lo_min > j0) j0 += (lo_min - j0) / kManyTile * kManyTile;   // tiles that no row sees are skipped
+        const int j_end = by_item ? hi_max : min(hi_max, base + step1 * STEP);
+        const int last = hi_max - 1;
+        const int32_t* table = a.step.table + (int64_t)pl.b * a.step.table_stride;
+        const uint8_t* kp = static_cast<const uint8_t*>(a.cache8.k) + (int64_t)h * a.cache8.head;
+        const uint8_t* vp = static_cast<const uint8_t*>(a.cache8.v) + (int64_t)h * a.cache8.head;
+        const float* ksp = a.cache8.k_scale + (int64_t)h * a.cache8.scale_head;
+        const float* vsp = a.cache8.v_scale + (int64_t)h * a.cache8.scale_head;
+        // Each lane looks one key of a tile up.  Those that no row of the tile sees are
+        // read as the nearest that one does.
+        int page = 0, in = 0;
+        auto look = [&](int j) {
+            const int t = min(max(j + lane, lo_min), last);
+            const int slot = (int)divide((uint32_t)t, a.by_page);
+            page = table[slot];
+            in = t - slot * a.cache8.page_size;
+        };
+        u32x4 raw[NI];
+        float ks_next = 0.f, vs_next = 0.f;       // of this lane's key
+        auto fetch = [&] {
+            const int g = min(max(page, 0), a.cache8.pages - 1);
+            const int64_t at = (int64_t)g * a.cache8.page + (int64_t)in * a.cache8.token;
+            const int64_t scale = (int64_t)g * a.cache8.scale_page + (int64_t)divide((uint32_t)in, a.by_block) * a.cache8.scale_block;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int n = i * T + (int)threadIdx.x, p = n & (NP - 1);
+                const uint8_t* from = n < NP ? kp : vp;
+                raw[i] = u32x4{};
+                const int64_t off = __shfl(at, p / PIECES);
+                if (FULL || (p % PIECES) * 16 < a.dim) raw[i] = *reinterpret_cast<const u32x4*>(from + off + (p % PIECES) * 16);
+            }
+            ks_next = ksp[scale];
+            vs_next = vsp[scale];
+        };
+        auto store = [&](int stage, bool folded) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int n = i * T + (int)threadIdx.x, p = n & (NP - 1), row = p / PIECES, piece = 2 * (p % PIECES);
+                const bool value = n >= NP;
+                const float f = __shfl(vs_next, row);
+                const float by = value && folded ? f : 1.f;
+                const int turn = value ? v_swizzle<DH>(row) : k_swizzle<DH>(row);
+                unsigned char* to = smem + stage * 2 * BYTES + (value ? BYTES : 0) + row * (DH * 2);
+                *reinterpret_cast<bf16x8*>(to + (piece ^ turn) * 16) = widen8(raw[i].x, raw[i].y, by);
+                *reinterpret_cast<bf16x8*>(to + ((piece + 1) ^ turn) * 16) = widen8(raw[i].z, raw[i].w, by);
+            }
+        };
+        float ks = 0.f, vs = 0.f;
+        bool folded = false;
+        auto take = [&](int stage) {              // the tile in registers becomes that of a stage
+            ks = ks_next;
+            vs = vs_next;
+            folded = __all(is_power(vs)) != 0;
+            store(stage, folded);
+        };
+        float ks_then = 0.f, vs_then = 0.f;       // of the stage that is being filled
+        bool folded_then = false;
+        if (j0 < j_end) {
+            look(j0);
+            fetch();
+            if (j0 + kManyTile < j_end) look(j0 + kManyTile);
+            take(0);
+            if (j0 + kManyTile < j_end) {
+                fetch();
+                if (j0 + 2 * kManyTile < j_end) look(j0 + 2 * kManyTile);
+            }
+        }
+        int stage = 0;
+        for (; j0 < j_end; j0 += kManyTile, stage ^= 1) {
+            __syncthreads();
+            if (j0 + kManyTile < j_end) {
+                const float k0 = ks, v0 = vs;
+                const bool f0 = folded;
+                take(stage ^ 1);
+                ks_then = ks;
+                vs_then = vs;
+                folded_then = folded;
+                ks = k0;
+                vs = v0;
+                folded = f0;
+                if (j0 + 2 * kManyTile < j_end) {
+                    fetch();
+                    if (j0 + 3 * kManyTile < j_end) look(j0 + 3 * kManyTile);
+                }
+            }
+            const unsigned char* kt = smem + stage * 2 * BYTES;
+            unsigned char* vt = smem + stage * 2 * BYTES + BYTES;
+
+            // a value that is not finite must not reach rows that do not see it, nor, by
+            // the weight 0 of a key past the ends (which holds a seen one's value),
+            // elements that are infinite
+            bool bad = false;
+            if (j0 < lo_max || j0 + kManyTile > hi_min) {
+                bool mine = false;
+                for (int i = threadIdx.x; i < BYTES / 16; i += T) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(vt + i * 16);
+                    mine |= not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
+                }
+                bad = __syncthreads_or(mine);
+            }
+            const bool idle = !works || j0 >= whi_max || j0 + kManyTile <= wlo_min;
+            if (!idle || bad) {
+                f32x16 sc[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) sc[x][v] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < KF; ++k) {
+                        const int row = 32 * x + col;
+                        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + row * (DH * 2) + ((2 * k + half) ^ k_swizzle<DH>(row)) * 16);
+                        sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], sc[x], 0, 0, 0);
+                    }
+                }
+                // Factors of the scores.  Those of keys that no row sees may be anything; 0
+                // would make NaN of -inf, which the smallest normal number does not.
+                const float by = fmaxf(ks * a.scale, 0x1p-126f);
+                float f[4];
+                if constexpr (UNI) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) f[g] = lane_of(by, 16 * g);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) sc[x][v] *= __shfl(by, 32 * x + 8 * (v / 4) + 4 * half + v % 4);
+                }
+                if (!full_rows || j0 < wlo_max || j0 + kManyTile > whi_min) {
+                    asm volatile("");      // a branch: most tiles need none of this
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const int j = j0 + 32 * x + 8 * (v / 4) + 4 * half + v % 4;
+                            sc[x][v] = j >= lo && j < hi ? sc[x][v] : minus_inf();
+                        }
+                }
+                float top = minus_inf();
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x16& y = sc[g / 2];
+                    const int v = 8 * (g % 2);
+                    float t = max3(y[v], y[v + 1], y[v + 2]);
+                    t = max3(t, y[v + 3], y[v + 4]);
+                    t = max3(t, y[v + 5], max3(y[v + 6], y[v + 7], y[v + 7]));
+                    top = max3(top, UNI ? t * f[g] : t, top);
+                }
+                top = max_halves(top);
+                // The maximum that a row's weights are relative to follows only when it is
+                // left behind by 2^8: sums scaled by less than that lose nothing.
+                const bool left = top - m > 8.f;
+                if (__any(left)) {
+                    const float keep = left ? exp2_(m - top) : 1.f;
+                    m = left ? top : m;
+                    l *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d] *= keep;
+                }
+                const float zero = m == minus_inf() ? 0.f : m;
+                u32x4 pb[4];
+                float sum[2] = {0.f, 0.f};
+                auto weights = [&](auto scaled) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int v = 0; v < 16; v += 2) {
+                            const int g = 2 * x + v / 8;
+                            float p = exp2_(UNI ? fmaf(sc[x][v], f[g], -zero) : sc[x][v] - zero);
+                            float q = exp2_(UNI ? fmaf(sc[x][v + 1], f[g], -zero) : sc[x][v + 1] - zero);
+                            sum[0] += p;
+                            sum[1] += q;
+                            if constexpr (decltype(scaled)::value) {
+                                // a key that is not seen may have any scale
+                                const int key = 32 * x + 8 * (v / 4) + 4 * half + v % 4;
+                                const float fp = UNI ? lane_of(vs, 16 * g) : __shfl(vs, key), fq = UNI ? fp : __shfl(vs, key + 1);
+                                p = p == 0.f ? 0.f : p * fp;
+                                q = q == 0.f ? 0.f : q * fq;
+                            }
+                            pb[2 * x + v / 8][v / 2 % 4] = pack_bf16(p, q);
+                        }
+                };
+                if (folded) weights(std::false_type{});
+                else weights(std::true_type{});
+                l += sum[0] + sum[1];
+                if (bad) {
+                    // such values go to the rows that see them, key by key, and count as
+                    // zeros in the product
+#pragma unroll 1
+                    for (int i = 0; i < kManyTile; ++i) {
+                        // key i lies in half (i / 4) % 2, element 4 ((i / 8) % 2) + i % 4 of pb[i / 16]
+                        uint32_t w = 0;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) w = x == i >> 4 && v == (i >> 3 & 1) * 2 + (i >> 1 & 1) ? pb[x][v] : w;
+                        w = __shfl(w, (i & 4) * 8 + col);
+                        const float p = from_bf16(i & 1 ? w >> 16 : w & 0xffffu);
+                        const bool sees = j0 + i >= lo && j0 + i < hi;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) {
+                                const int e = 32 * d + 8 * v + 4 * half;
+                                const uint16_t* q = reinterpret_cast<const uint16_t*>(vt + i * (DH * 2) + ((e / 8) ^ v_swizzle<DH>(i)) * 16) + e % 8;
+#pragma unroll
+                                for (int y = 0; y < 4; ++y) {
+                                    const float z = fmaf(p, from_bf16(q[y]), o[d][4 * v + y]);
+                                    o[d][4 * v + y] = sees && not_finite(q[y]) ? z : o[d][4 * v + y];
+                                }
+                            }
+                    }
+                    __syncthreads();
+                    for (int i = threadIdx.x; i < BYTES / 2; i += T) {
+                        uint16_t* q = reinterpret_cast<uint16_t*>(vt) + i;
+                        if (not_finite(*q)) *q = 0;
+                    }
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        s16x8 vf;
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int row = 16 * c + 8 * y + 4 * half + (lane & 15) / 4;
+                            const int e = 32 * d + (lane & 16) + 4 * (lane & 3);
+                            const unsigned char* q = vt + row * (DH * 2) + ((e / 8) ^ v_swizzle<DH>(row)) * 16 + (e % 8) * 2;
+                            const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) vf[4 * y + v] = t[v];
+                        }
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pb[c]), o[d], 0, 0, 0);
+                    }
+            }
+            ks = ks_then;
+            vs = vs_then;
+            folded = folded_then;
+        }
+
+        // ---- results: a lane holds 4 elements after another of its row -------------------
+        l += __shfl_xor(l, 32);
+        float top = m;
+        bool finish = whole;
+        if (STEP != 0 && !whole) {
+            // a part in the order of this kernel's registers, two floats of a lane at a
+            // time beside those of its neighbours
+            constexpr int F = kPartFloats<DH, ROWS>;
+            const int64_t begin = pl.first + (int64_t)item * pl.steps;
+            const Parts parts = parts_of(begin, begin + pl.steps, all.share);
+            const int at = wave * kManyRows * DH + 2 * lane;
+            finish = others_done(a, parts, &flag);
+            if (!finish) {
+                float* part = part_at<F>(a, parts, parts.mine);
+                if (works) {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int v = 0; v < 16; v += 2) put2(part + at + (d * 8 + v / 2) * 128, o[d][v], o[d][v + 1]);
+                    if (half == 0) put2(part + ROWS * DH + 2 * my, top, l);
+                }
+                finish = last_to_arrive(a, parts, &flag);
+            }
+            if (finish) {
+                if (works) {
+                    // all parts in their order, this workgroup's from its registers
+                    float most = top;
+                    for (int i = 0; i < parts.count; ++i)
+                        if (i != parts.mine) most = fmaxf(most, get2(part_at<F>(a, parts, i) + ROWS * DH + 2 * my).x);
+                    const float z = most == minus_inf() ? 0.f : most;
+                    float l_all = 0.f;
+                    f32x16 o_all[DT];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) o_all[d][v] = 0.f;
+                    for (int i = 0; i < parts.count; ++i) {
+                        const float* part = part_at<F>(a, parts, i);
+                        if (i == parts.mine) {
+                            const float f = exp2_(top - z);
+                            l_all = fmaf(l, f, l_all);
+#pragma unroll
+                            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) o_all[d][v] = fmaf(o[d][v], f, o_all[d][v]);
+                        } else {
+                            const float2 ml = get2(part + ROWS * DH + 2 * my);
+                            const float f = exp2_(ml.x - z);
+                            l_all = fmaf(ml.y, f, l_all);
+#pragma unroll
+                            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                for (int v = 0; v < 16; v += 2) {
+                                    const float2 x = get2(part + at + (d * 8 + v / 2) * 128);
+                                    o_all[d][v] = fmaf(x.x, f, o_all[d][v]);
+                                    o_all[d][v + 1] = fmaf(x.y, f, o_all[d][v + 1]);
+                                }
+                        }
+                    }
+                    top = most;
+                    l = l_all;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d] = o_all[d];
+                }
+                joined(a, parts);
+            }
+        }
+        if (finish && live) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float acc[4] = {o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]};
+                    finish_row<4>(a, s.q0 + tok, head, 32 * d + 8 * v + 4 * half, acc, l, top);
+                }
+        }
+        if constexpr (STEP == 0) return;
+        __syncthreads();      // the tiles in shared memory are free
+        u += by_item ? -(int64_t)gridDim.x : (int64_t)(step1 - step0);
+    }
+}
+
 // ---- launches ------------------------------------------------------------------------------
 // Whether 16 tokens from a multiple of 16 on lie in one page and block, a page below 2 GB.
 bool in_halves(const Attend8Args& a)
@@ -421,14 +844,49 @@ hipError_t few(const Attend8Args& a, hipStream_t s)
     return pg16 ? launch(attend8_few_kernel<DH, RT, true, false>) : launch(attend8_few_kernel<DH, RT, false, false>);
 }
 
+// Wavefronts of a workgroup of the kernel for many rows.
+template <int DH>
+constexpr int kManyWaves = DH == 256 ? 4 : 8;
+constexpr int kManyStep = 256;
+
+template <int DH>
+hipError_t many(const Attend8Args& a, hipStream_t s)
+{
+    constexpr int NW = kManyWaves<DH>, ROWS = NW * kManyRows;
+    // no more items than this, whatever the sequences' lengths
+    const int64_t items = ((a.tokens * a.group + ROWS - 1) / ROWS + a.step.seqs) * a.kv_heads;
+    auto launch = [&](auto kernel, int64_t groups) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(NW * 64), 0, s, a);
+        return hipGetLastError();
+    };
+    const bool uni = a.cache8.page_size % 16 == 0 && a.cache8.block % 16 == 0;
+    // An item a workgroup where that makes two rounds at least, else a workgroup a CU
+    // and shares of the steps, as in the bf16 kernel.  A launch has fewer than 2^32
+    // threads.
+    if ((a.tokens * a.group / ROWS) * a.kv_heads >= 2 * a.cus && a.step.seqs <= kSearched && items * (NW * 64) <= (int64_t)UINT32_MAX) {
+        if (a.dim == DH) return uni ? launch(attend8_many_kernel<DH, NW, 0, true, true>, items) : launch(attend8_many_kernel<DH, NW, 0, false, true>, items);
+        return uni ? launch(attend8_many_kernel<DH, NW, 0, true, false>, items) : launch(attend8_many_kernel<DH, NW, 0, false, false>, items);
+    }
+    if (a.dim == DH)
+        return uni ? launch(attend8_many_kernel<DH, NW, kManyStep, true, true>, a.cus) : launch(attend8_many_kernel<DH, NW, kManyStep, false, true>, a.cus);
+    return uni ? launch(attend8_many_kernel<DH, NW, kManyStep, true, false>, a.cus) : launch(attend8_many_kernel<DH, NW, kManyStep, false, false>, a.cus);
+}
+
 template <int DH>
 hipError_t attend8(const Attend8Args& args, hipStream_t s)
 {
     Attend8Args a = args;
-    a.scale = a.raw_scale * kLog2e;
     const int64_t rows = a.tokens * a.group;
-    if (rows <= 16 * (int64_t)a.step.seqs) return few<DH, 1>(a, s);
-    return few<DH, DH == 256 ? 2 : 4>(a, s);
+    if (rows <= 64 * (int64_t)a.step.seqs) {
+        a.scale = a.raw_scale * kLog2e;
+        if (rows <= 16 * (int64_t)a.step.seqs) return few<DH, 1>(a, s);
+        return few<DH, DH == 256 ? 2 : 4>(a, s);
+    }
+    a.scale = fabsf(a.raw_scale) * kLog2e;
+    a.flip = a.raw_scale < 0.f ? 0x80008000u : 0u;
+    a.keep = a.scale > 0.f ? ~0u : 0u;
+    if (!a.keep) a.scale = 1.f;
+    return many<DH>(a, s);
 }
 
 }  // namespace

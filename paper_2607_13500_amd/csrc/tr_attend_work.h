@@ -303,6 +303,17 @@ __device__ __forceinline__ int v_piece(int row, int piece)
 // 16 bytes of keys or values that nothing reads again soon.
 __device__ __forceinline__ u32x4 read_once(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4*>(p)); }
 
+// ---- tiles of many rows ---------------------------------------------------------------
+constexpr int kManyTile = 64, kManyRows = 32;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int DH>
+__device__ __forceinline__ int v_swizzle(int row)
+{
+    return DH == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
+}
+
 // Whether the workgroups take whole items in turn instead of equal shares of all
 // steps.  Shares count an item's steps as those of all its sequence's rows; where
 // tiles see only part of them (a prompt's, half of them on average; those under a
