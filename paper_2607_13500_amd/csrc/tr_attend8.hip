@@ -22,6 +22,11 @@ typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 __device__ __forceinline__ float lane_of(float x, int i) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), i)); }
 
+__device__ __forceinline__ int64_t lane_of(int64_t x, int i)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, i));
+}
+
 // Eight e4m3 values as bf16, times a power of two.
 __device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float by = 1.f)
 {
@@ -49,19 +54,21 @@ __device__ __forceinline__ int piece8(int row, int piece)
 }
 
 // ---- few rows over many keys -----------------------------------------------------------
-// Items are RT tiles of 16 rows, steps kStep keys; the four wavefronts take tiles of 32
-// keys in turn, as in the bf16 kernel, and what is widened of a tile serves all its rows.
-constexpr int kTile = 32, kStep = 128;
+// Items are RT tiles of 16 rows, steps 4 kTile keys; the four wavefronts take tiles of
+// kTile keys in turn, as in the bf16 kernel, and what is widened of a tile serves all its rows.
+template <int DH>
+constexpr int kFewTile = DH == 64 ? 64 : 32;
 
 template <int DH, int RT>
-constexpr int kFewPerCu8 = DH == 256 ? 1 : RT == 4 ? 1 : 2;
+constexpr int kFewPerCu8 = DH == 256 ? 1 : RT == 4 ? (DH == 64 ? 2 : 1) : RT == 2 ? 2 : 3;
 
 // PG16: pages and blocks of whole halves of a tile (multiples of 16 tokens, pages below
 // 2 GB), so that a half's page and scales are the wavefront's.  FULL: head_dim is DH.
 template <int DH, int RT, bool PG16, bool FULL>
 __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few_kernel(Attend8Args a)
 {
-    constexpr int ROWS = 16 * RT;
+    constexpr int ROWS = 16 * RT, kTile = kFewTile<DH>, kStep = 4 * kTile;
+    constexpr int X = kTile / 16, C = kTile / 32;      // sixteens of keys and fragments of weights of a tile
     constexpr int KF = DH / 32, DT = DH / 16;          // fragments of keys, tiles of elements
     constexpr int PIECES = DH / 16, VR = 64 / PIECES, VN = kTile / VR;   // pieces of a row, rows of a load, loads of a tile
     constexpr int PAD = DH + 4;
@@ -77,7 +84,7 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
     unsigned char* kt = smem + wave * 2 * BYTES;                 // the wavefront's tile
     unsigned char* vt = kt + BYTES;
     const int token_bytes = (int)a.cache8.token;                 // PG16
-    const int in_lane = vrow * token_bytes + piece * 16;
+    const uint32_t in_lane = (uint32_t)(vrow * token_bytes + piece * 16);
 
     const Shares all = shares_of<ROWS, kStep>(a, lane);
     int64_t u = (int64_t)blockIdx.x * all.share;
@@ -132,7 +139,7 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
         }
 
         // ---- keys -------------------------------------------------------------------
-        const int base = s.begin & ~(kTile - 1);
+        const int base = s.begin & ~(kAlign - 1);
         const int j_end = min(hi_max, base + step1 * kStep);
         const int first = base + step0 * kStep + wave * kTile;
         // tiles before any row's range are skipped
@@ -146,58 +153,76 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
         const float* vsp = a.cache8.v_scale + (int64_t)h * a.cache8.scale_head;
         const int last = hi_max - 1;              // tokens past it (and before lo_min) are read as it (as lo_min)
 
-        auto page_at = [&](int slot) { return min(max(table[slot], 0), a.cache8.pages - 1); };
         u32x4 kr[VN], vr[VN];
-        float ks[2], vs[2];                       // PG16: of the tile's halves, else of this lane's token of each
+        // PG16: each lane looks up sixteen keys, all lanes those of the next BT tiles, of
+        // which a tile's are the wavefront's when its turn comes.  Rows of a sixteen that no row
+        // sees are read all the same (they are in the page), one without any in the
+        // place of the nearest one.
+        // Else a lane looks up a key of one tile, a tile ahead.
+        constexpr int BT = 64 / X;
+        int page = 0, in = 0, ahead = 0;          // ahead: tiles that are looked up and not fetched
+        int64_t off = 0;
+        float ks = 0.f, vs = 0.f, ks_next[X], vs_next[X];
+        auto look = [&](int j) {
+            const int t = PG16 ? min(max(j + (lane / X) * kStep + (lane % X) * 16, lo_min & ~15), last & ~15)
+                               : min(max(j + (lane & (kTile - 1)), lo_min), last);
+            const int slot = (int)divide((uint32_t)t, a.by_page);
+            page = table[slot];
+            in = t - slot * a.cache8.page_size;
+        };
+        auto find = [&] {
+            const int g = min(max(page, 0), a.cache8.pages - 1);
+            off = (int64_t)g * a.cache8.page + (int64_t)in * a.cache8.token;
+            const int64_t scale = (int64_t)g * a.cache8.scale_page + (int64_t)divide((uint32_t)in, a.by_block) * a.cache8.scale_block;
+            ks = ksp[scale];
+            vs = vsp[scale];
+        };
         auto fetch = [&](int j) {
             if constexpr (PG16) {
+                if (ahead == 0) {
+                    look(j);
+                    find();
+                    ahead = BT;
+                }
+                const int at = (BT - ahead) * X;
+                --ahead;
+                constexpr int EACH = VN / X;
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    // rows of a half that no row sees are read all the same (they are in
-                    // the page), a half without any in the place of the nearest one
-                    const int half = min(max(j + 16 * x, lo_min & ~15), last & ~15);
-                    const int slot = (int)divide((uint32_t)half, a.by_page), in = half - slot * a.cache8.page_size;
-                    const int page = __builtin_amdgcn_readfirstlane(page_at(slot));
-                    const int64_t off = uniform((int64_t)page * a.cache8.page + (int64_t)in * a.cache8.token);
-                    const int64_t scale = uniform((int64_t)page * a.cache8.scale_page + (int64_t)divide((uint32_t)in, a.by_block) * a.cache8.scale_block);
-                    ks[x] = ksp[scale];
-                    vs[x] = vsp[scale];
-                    const unsigned char* kb = kp + off + in_lane;
-                    const unsigned char* vb = vp + off + in_lane;
-                    constexpr int HALF = VN >= 2 ? VN / 2 : 1;
+                for (int x = 0; x < X; ++x) {
+                    ks_next[x] = lane_of(ks, at + x);
+                    vs_next[x] = lane_of(vs, at + x);
+                    const int64_t o = lane_of(off, at + x);
 #pragma unroll
-                    for (int i = 0; i < HALF; ++i)
+                    for (int i = 0; i < EACH; ++i) {
+                        const uint8_t* kb = kp + o + (int64_t)i * VR * token_bytes;      // the wavefront's
+                        const uint8_t* vb = vp + o + (int64_t)i * VR * token_bytes;
                         if (FULL || piece * 16 < a.dim) {
-                            kr[x * HALF + i] = read_once(kb + i * VR * token_bytes);
-                            vr[x * HALF + i] = read_once(vb + i * VR * token_bytes);
+                            kr[x * EACH + i] = read_once(kb + in_lane);
+                            vr[x * EACH + i] = read_once(vb + in_lane);
                         }
-                }
-            } else {
-                int64_t koff[2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int t = min(max(j + 16 * x + col, lo_min), last);
-                    const int slot = (int)divide((uint32_t)t, a.by_page), in = t - slot * a.cache8.page_size, page = page_at(slot);
-                    koff[x] = (int64_t)page * a.cache8.page + (int64_t)in * a.cache8.token;
-                    const int64_t scale = (int64_t)page * a.cache8.scale_page + (int64_t)divide((uint32_t)in, a.by_block) * a.cache8.scale_block;
-                    ks[x] = ksp[scale];
-                    vs[x] = vsp[scale];
-                }
-#pragma unroll
-                for (int i = 0; i < VN; ++i) {
-                    const int64_t off = __shfl(koff[VR * i / 16], (VR * i + vrow) & 15) + piece * 16;
-                    if (FULL || piece * 16 < a.dim) {
-                        kr[i] = read_once(kp + off);
-                        vr[i] = read_once(vp + off);
                     }
                 }
+            } else {
+                find();
+#pragma unroll
+                for (int i = 0; i < VN; ++i) {
+                    const int64_t o = __shfl(off, VR * i + vrow) + piece * 16;
+                    if (FULL || piece * 16 < a.dim) {
+                        kr[i] = read_once(kp + o);
+                        vr[i] = read_once(vp + o);
+                    }
+                }
+                if (j + kStep < j_end) look(j + kStep);
             }
         };
         if constexpr (!FULL) {
 #pragma unroll
             for (int i = 0; i < VN; ++i) kr[i] = vr[i] = u32x4{};   // pieces past the head stay zero
         }
-        if (j0 < j_end) fetch(j0);
+        if (j0 < j_end) {
+            if constexpr (!PG16) look(j0);
+            fetch(j0);
+        }
         for (; j0 < j_end; j0 += kStep) {
             // rows that see different tokens of this tile: a NaN must not reach the rows
             // that do not see it
@@ -221,11 +246,17 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
                 *reinterpret_cast<u32x4*>(kt + row * DH + piece8<DH>(row, piece) * 16) = kr[i];
                 *reinterpret_cast<u32x4*>(vt + row * DH + piece8<DH>(row, piece) * 16) = vr[i];
             }
-            const float ks0[2] = {ks[0], ks[1]}, vs0[2] = {vs[0], vs[1]};
-            if (j0 + kStep < j_end) fetch(j0 + kStep);
-            f32x4 sc[RT][2];
+            float ks_tile[X], vs_tile[X];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
+            for (int x = 0; x < X; ++x) {
+                ks_tile[x] = ks_next[x];
+                vs_tile[x] = vs_next[x];
+            }
+            const float ks_lane = ks, vs_lane = vs;
+            if (j0 + kStep < j_end) fetch(j0 + kStep);
+            f32x4 sc[RT][X];
+#pragma unroll
+            for (int x = 0; x < X; ++x) {
 #pragma unroll
                 for (int i = 0; i < RT; ++i) sc[i][x] = f32x4{0.f, 0.f, 0.f, 0.f};
                 const int row = 16 * x + col;
@@ -242,21 +273,27 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
             }
 
             // ---- weights ------------------------------------------------------------
-            float kf[8], vf[8];                   // scales of this lane's keys
+            float kf[4 * X], vf[4 * X];           // scales of this lane's keys
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < X; ++x)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    kf[4 * x + v] = (PG16 ? ks0[x] : __shfl(ks0[x], 4 * grp + v)) * a.scale;
-                    vf[4 * x + v] = PG16 ? vs0[x] : __shfl(vs0[x], 4 * grp + v);
+                    kf[4 * x + v] = (PG16 ? ks_tile[x] : __shfl(ks_lane, 16 * x + 4 * grp + v)) * a.scale;
+                    vf[4 * x + v] = PG16 ? vs_tile[x] : __shfl(vs_lane, 16 * x + 4 * grp + v);
                 }
-            u32x4 pb[RT];
+            u32x4 pb[RT][C];
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                float p[8];
+                // Tiles without rows are left out of the weights, but not of the products: a
+                // branch may not lie between a matrix instruction and a reader of its result,
+                // whose wait the compiler then does not count on every way there.
+#pragma unroll
+                for (int c = 0; c < C; ++c) pb[i][c] = u32x4{};
+                if (i > 0 && 16 * i >= rows) continue;
+                float p[4 * X];
                 float top = minus_inf();
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int x = 0; x < X; ++x)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const int j = j0 + 16 * x + 4 * grp + v;
@@ -272,13 +309,13 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
                 m[i] = m1;
                 l[i] *= keep;
 #pragma unroll
-                for (int v = 0; v < 8; ++v) {
+                for (int v = 0; v < 4 * X; ++v) {
                     p[v] = exp2_(p[v] - zero);
                     l[i] += p[v];
                     p[v] = p[v] == 0.f ? 0.f : p[v] * vf[v];      // a token that is not seen may have any scale
                 }
 #pragma unroll
-                for (int v = 0; v < 4; ++v) pb[i][v] = pack_bf16(p[2 * v], p[2 * v + 1]);
+                for (int v = 0; v < 2 * X; ++v) pb[i][v / 4][v % 4] = pack_bf16(p[2 * v], p[2 * v + 1]);
                 if (!__all(same)) {
 #pragma unroll
                     for (int d = 0; d < DT; ++d) o[i][d] *= keep;
@@ -307,16 +344,19 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
                         if (is_nan8(vt[t * DH + e])) vt[t * DH + e] = 0;
             }
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                // eight keys of an element to a lane: those of its weights
-                const int n = (lane & 15) >> 1, row = 4 * grp + (n & 3) + 16 * (n >> 2);
-                const unsigned char* q = vt + row * DH + piece8<DH>(row, d) * 16 + (lane & 1) * 8;
-                const i32x2 t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)q);
-                const bf16x8 w = widen8((uint32_t)t.x, (uint32_t)t.y);
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int i = 0; i < RT; ++i)
-                    o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, pb[i]), o[i][d], 0, 0, 0);
-            }
+                for (int d = 0; d < DT; ++d) {
+                    // eight keys of an element to a lane: those of its weights
+                    const int n = (lane & 15) >> 1, row = 32 * c + 4 * grp + (n & 3) + 16 * (n >> 2);
+                    const unsigned char* q = vt + row * DH + piece8<DH>(row, d) * 16 + (lane & 1) * 8;
+                    const i32x2 t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)q);
+                    const bf16x8 w = widen8((uint32_t)t.x, (uint32_t)t.y);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, pb[i][c]), o[i][d], 0, 0, 0);
+                    }
+                }
         }
 
         // ---- the four wavefronts' parts, a tile of rows after another --------------------
@@ -365,8 +405,8 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
             }
         }
         if (!whole && last_to_arrive(a, parts, &flag)) {
-            // all parts in their order, eight of them on their way at a time
-            constexpr int U = N > 8 ? 4 : 8;
+            // all parts in their order, four of them on their way at a time
+            constexpr int U = 4;
             for (int mine = row; mine < rows; mine += 16) {
                 float top = minus_inf(), sum = 0.f, acc[N] = {};
                 for (int i0 = 0; i0 < parts.count; i0 += U) {
@@ -880,7 +920,8 @@ hipError_t attend8(const Attend8Args& args, hipStream_t s)
     if (rows <= 64 * (int64_t)a.step.seqs) {
         a.scale = a.raw_scale * kLog2e;
         if (rows <= 16 * (int64_t)a.step.seqs) return few<DH, 1>(a, s);
-        return few<DH, DH == 256 ? 2 : 4>(a, s);
+        if (rows <= 32 * (int64_t)a.step.seqs || DH == 256) return few<DH, 2>(a, s);
+        if constexpr (DH < 256) return few<DH, 4>(a, s);
     }
     a.scale = fabsf(a.raw_scale) * kLog2e;
     a.flip = a.raw_scale < 0.f ? 0x80008000u : 0u;
