@@ -586,7 +586,7 @@ tr_status tr_update_pages(int32_t seqs, const int32_t* change, const int32_t* kv
  * outside [0, vocab) are rejected.  Products, differences and sums are in 64 bits.
  *   target, draft  device [T, vocab] of dtype, rows ld elements apart (>= vocab)
  *   ids            device int32 [T]; accept device float [T]; draw device float [seqs]
- *   scratch        device, tr_verify_scratch(seqs) bytes, 8-byte aligned, of one
+ *   scratch        device, tr_verify_scratch(seqs) bytes, 16-byte aligned, of one
  *                  call at a time; its contents mean nothing before and after
  * q_start is not checked by the host: rows outside [0, T) are never read. */
 size_t tr_verify_scratch(int32_t seqs);

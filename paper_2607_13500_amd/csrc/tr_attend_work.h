@@ -4,6 +4,7 @@
 #pragma once
 
 #include "tr_attn.h"
+#include "tr_divide.h"
 #include "tr_wave.h"
 
 namespace tr {
@@ -49,9 +50,6 @@ __device__ __forceinline__ bool not_finite(uint32_t w)
 }
 
 // ---- sequences ---------------------------------------------------------------------
-// j / page_size and r / group for uniform divisors, by multiplication.
-__device__ __forceinline__ uint32_t divide(uint32_t x, const Divisor& d) { return (__umulhi(d.mul, x) + x) >> d.shift; }
-
 // One sequence of the step, its fields clamped to what the tensors hold.
 struct Sequence {
     int64_t q0;        // first packed row
@@ -371,16 +369,6 @@ __device__ __forceinline__ float max_halves(float x)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-// ---- launches ------------------------------------------------------------------------------
-[[maybe_unused]] inline Divisor divisor(uint32_t d)
-{
-    Divisor v;
-    v.shift = 0;
-    while ((1ull << v.shift) < d) ++v.shift;
-    v.mul = (uint32_t)(((1ull << 32) * ((1ull << v.shift) - d)) / d + 1);
-    return v;
 }
 
 }  // namespace

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "tr.h"
+#include "tr_divide.h"
 
 namespace tr {
 
@@ -72,11 +73,6 @@ hipError_t launch_rotate(const RotateArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_rotate_backward(const RotateArgs& a, bool bf16, hipStream_t s);
 
 // ---- attention ---------------------------------------------------------------
-// Division of x < 2^31 by a number fixed for a launch: (mulhi(x, mul) + x) >> shift.
-struct Divisor {
-    uint32_t mul, shift;
-};
-
 struct AttendArgs {
     int64_t tokens;
     int32_t heads, kv_heads, dim;

@@ -12,156 +12,174 @@
 #include <algorithm>
 
 #include "tr_step.h"
+#include "tr_wave.h"
 
 namespace tr {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int32_t kImpossible = INT32_MAX;
 
+// Sums that stay at 2^32 - 1 once they are past it: more than any pool or batch of rows.
 struct Sums {
-    int64_t fresh, take, give;   // new tokens, pages taken and given back
+    uint32_t fresh, take, give;   // new tokens, pages taken and given back
 };
 
-__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) { return {x.fresh + y.fresh, x.take + y.take, x.give + y.give}; }
+__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y)
+{
+    return {__builtin_elementwise_add_sat(x.fresh, y.fresh), __builtin_elementwise_add_sat(x.take, y.take),
+            __builtin_elementwise_add_sat(x.give, y.give)};
+}
 
 // One sequence: its lengths, its pages before and after, and whether they fit.
 struct Sequence {
-    int64_t length;
-    int64_t held, need;
+    int32_t length, held, need;
     Sums sums;
     bool fits;
 };
+
+__device__ __forceinline__ int32_t pages_for(const PagesArgs& a, int32_t n)
+{
+    return n ? (int32_t)divide((uint32_t)n - 1, a.by_page) + 1 : 0;
+}
 
 __device__ __forceinline__ Sequence sequence_of(const PagesArgs& a, int b)
 {
     Sequence s{};
     s.fits = true;
     if (b >= a.seqs) return s;
-    const int64_t kv = max(a.kv_len[b], 0), change = a.change[b];
-    s.length = max(kv + change, (int64_t)0);
-    s.held = (kv + a.page_size - 1) / a.page_size;
-    s.need = (s.length + a.page_size - 1) / a.page_size;
-    s.sums = {max(change, (int64_t)0), max(s.need - s.held, (int64_t)0), max(s.held - s.need, (int64_t)0)};
-    s.fits = s.length <= INT32_MAX && max(s.held, s.need) <= a.table_width;
+    const int32_t kv = max(a.kv_len[b], 0), change = a.change[b];
+    const int64_t length = max((int64_t)kv + change, (int64_t)0);
+    s.length = (int32_t)min(length, (int64_t)INT32_MAX);
+    s.held = pages_for(a, kv);
+    s.need = pages_for(a, s.length);
+    s.sums = {(uint32_t)max(change, 0), (uint32_t)max(s.need - s.held, 0), (uint32_t)max(s.held - s.need, 0)};
+    s.fits = length <= INT32_MAX && max(s.held, s.need) <= a.table_width;
     return s;
 }
 
-// Inclusive sums over the workgroup's threads, and the whole sum in `all`.
-__device__ __forceinline__ Sums scan(Sums x, Sums& all, Sums (&shared)[kWaves])
+// Inclusive sums over the workgroup's T threads, and the whole sum in `all`.
+template <int T>
+__device__ __forceinline__ Sums scan(Sums x, Sums& all, uint4 (&shared)[T / 64])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const Sums y = {__shfl_up(x.fresh, m), __shfl_up(x.take, m), __shfl_up(x.give, m)};
-        if (lane >= m) x = x + y;
-    }
-    if (lane == 63) shared[wave] = x;
+    auto add = [&](int m) { x = x + Sums{dpp_u32(x.fresh, m), dpp_u32(x.take, m), dpp_u32(x.give, m)}; };
+    add(1);
+    add(2);
+    add(4);
+    add(8);
+    add(15);
+    add(31);
+    if (lane == 63) shared[wave] = uint4{x.fresh, x.take, x.give, 0};
     __syncthreads();
     Sums before{};
     all = {};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before = before + shared[w];
-        all = all + shared[w];
+    for (int w = 0; w < T / 64; ++w) {
+        const uint4 y = shared[w];
+        if (w < wave) before = before + Sums{y.x, y.y, y.z};
+        all = all + Sums{y.x, y.y, y.z};
     }
     __syncthreads();
     return x + before;
 }
 
-// First of the n ends that is above x.
-__device__ __forceinline__ int find(const int32_t* ends, int n, int32_t x)
+// First of a chunk's T ends that is above x, which is below the last one's.
+template <int T>
+__device__ __forceinline__ int find(const uint32_t* ends, uint32_t x)
 {
     int lo = 0;
-    for (int step = kThreads; step; step >>= 1)
-        if (lo + step <= n && ends[lo + step - 1] <= x) lo += step;
+#pragma unroll
+    for (int step = T / 2; step; step >>= 1)
+        if (ends[lo + step - 1] <= x) lo += step;
     return lo;
 }
 
-// A workgroup's share [first, last) of n things, cut down to [c0, c1).
+// A workgroup's share [first, last) of n < 2^31 things, cut down to [c0, c1).
 struct Range {
-    int32_t first, last;
+    uint32_t first, last;
 };
 
-__device__ __forceinline__ Range share(int64_t n, int64_t c0, int64_t c1)
+__device__ __forceinline__ Range share(uint32_t n, uint32_t c0, uint32_t c1)
 {
-    const int64_t each = (n + gridDim.x - 1) / gridDim.x;
-    return {(int32_t)max(blockIdx.x * each, c0), (int32_t)min(min((blockIdx.x + 1) * each, n), c1)};
+    const uint32_t each = (n + gridDim.x - 1) / gridDim.x;
+    return {max(min(blockIdx.x * each, n), c0), min(min((blockIdx.x + 1) * each, n), c1)};
 }
 
 // `tables`: rows, pages, slots and places; `lengths`: kv_out and state_out, by the
 // first workgroup (which may be kv_len and state, that other workgroups still read).
-__global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a, bool tables, bool lengths)
+template <int T>
+__global__ __launch_bounds__(T) void pages_kernel(PagesArgs a, bool tables, bool lengths)
 {
-    __shared__ Sums shared[kWaves];
-    __shared__ int32_t fresh_end[kThreads], take_end[kThreads], give_end[kThreads];
-    __shared__ int32_t length[kThreads], held[kThreads], need[kThreads];
+    __shared__ uint4 shared[T / 64];
+    __shared__ uint32_t fresh_end[T], take_end[T], give_end[T];
+    __shared__ int32_t length[T], held[T], need[T];
     const int tid = threadIdx.x;
-    const uint32_t pages = (uint32_t)a.pages;
-    const int64_t first = min(max(a.state[0], 0), a.pages - 1), free = min(max(a.state[1], 0), a.pages);
+    const int32_t state0 = a.state[0], state1 = a.state[1];
+    const uint32_t pages = (uint32_t)a.pages, first = (uint32_t)min(max(state0, 0), a.pages - 1), free = (uint32_t)min(max(state1, 0), a.pages);
+    auto in_ring = [&](uint32_t i) { return i >= pages ? i - pages : i; };       // i < 2 pages
 
     // ---- the whole step -------------------------------------------------------------
     Sums all{};
     bool fits = true;
     Sequence s{};
     Sums mine{};
-    for (int b0 = 0; b0 < a.seqs; b0 += kThreads) {
+    for (int b0 = 0; b0 < a.seqs; b0 += T) {
         s = sequence_of(a, b0 + tid);
         fits = fits && s.fits;
         Sums sum;
-        mine = scan(s.sums, sum, shared);
+        mine = scan<T>(s.sums, sum, shared);
         all = all + sum;
     }
     fits = __syncthreads_and(fits);
     int32_t lacking = 0;
-    if (!fits || all.fresh > a.rows || free + all.give > a.pages) lacking = kImpossible;
-    else if (all.take > free) lacking = (int32_t)(all.take - free);
-    const bool done = lacking == 0, one = a.seqs <= kThreads;
+    if (!fits || all.fresh > (uint32_t)a.rows || all.give > pages - free) lacking = kImpossible;
+    else if (all.take > free) lacking = (int32_t)min(all.take - free, (uint32_t)kImpossible);
+    const bool done = lacking == 0, one = a.seqs <= T;
 
     // ---- sequences, a chunk at a time -------------------------------------------------
     Sums before{};
-    for (int b0 = 0; b0 < a.seqs; b0 += kThreads) {
-        const int b = b0 + tid, n = min(kThreads, a.seqs - b0);
+    for (int b0 = 0; b0 < a.seqs; b0 += T) {
+        const int b = b0 + tid, n = min(T, a.seqs - b0);
         Sums sum = all;
         if (!one) {
             s = sequence_of(a, b);
-            mine = scan(s.sums, sum, shared);
+            mine = scan<T>(s.sums, sum, shared);
         }
-        const Sums end = before + mine;
+        const Sums end = before + mine, past = before + sum;
         if (tid < n) {
-            if (lengths && blockIdx.x == 0) a.kv_out[b] = done ? (int32_t)s.length : a.kv_len[b];
+            if (lengths && blockIdx.x == 0) a.kv_out[b] = done ? s.length : a.kv_len[b];
             if (tables && blockIdx.x == 0) a.q_start[b + 1] = done ? (int32_t)end.fresh : 0;
         }
-        if (!done || !tables) continue;
-        fresh_end[tid] = (int32_t)end.fresh;
-        take_end[tid] = (int32_t)end.take;
-        give_end[tid] = (int32_t)end.give;
-        length[tid] = (int32_t)s.length;
-        held[tid] = (int32_t)s.held;
-        need[tid] = (int32_t)s.need;
+        if (!done || !tables) {
+            before = past;
+            continue;
+        }
+        fresh_end[tid] = end.fresh;           // threads without a sequence: the last one's
+        take_end[tid] = end.take;
+        give_end[tid] = end.give;
+        length[tid] = s.length;
+        held[tid] = s.held;
+        need[tid] = s.need;
         __syncthreads();
-        const Sums past = before + sum;
         const Range takes = share(all.take, before.take, past.take);
-        for (int32_t k = takes.first + tid; k < takes.last; k += kThreads) {
-            const int i = find(take_end, n, k);
-            const int32_t slot = need[i] - (take_end[i] - k);
-            a.table[(b0 + i) * a.table_stride + slot] = a.ring[(uint32_t)(first + k) % pages];
+        for (uint32_t k = takes.first + tid; k < takes.last; k += T) {
+            const int i = find<T>(take_end, k);
+            a.table[(b0 + i) * a.table_stride + need[i] - (int32_t)(take_end[i] - k)] = a.ring[in_ring(first + k)];
         }
         const Range gives = share(all.give, before.give, past.give);
-        for (int32_t k = gives.first + tid; k < gives.last; k += kThreads) {
-            const int i = find(give_end, n, k);
-            const int32_t slot = held[i] - (give_end[i] - k);
-            a.ring[(uint64_t)(first + free + k) % pages] = a.table[(b0 + i) * a.table_stride + slot];
+        for (uint32_t k = gives.first + tid; k < gives.last; k += T) {
+            const int i = find<T>(give_end, k);
+            a.ring[in_ring(in_ring(first + free) + k)] = a.table[(b0 + i) * a.table_stride + held[i] - (int32_t)(give_end[i] - k)];
         }
-        const Range tokens = share(a.rows, before.fresh, past.fresh);
-        for (int32_t t = tokens.first + tid; t < tokens.last; t += kThreads) {
-            const int i = find(fresh_end, n, t);
-            const int32_t p = length[i] - (fresh_end[i] - t), slot = p / a.page_size;
+        const Range tokens = share((uint32_t)a.rows, before.fresh, past.fresh);
+        for (uint32_t t = tokens.first + tid; t < tokens.last; t += T) {
+            const int i = find<T>(fresh_end, t);
+            const int32_t p = length[i] - (int32_t)(fresh_end[i] - t), slot = (int32_t)divide((uint32_t)p, a.by_page);
             if (a.pos) a.pos[t] = p;
             if (a.slots) {
                 const int32_t taken = slot - held[i];
-                const int32_t page = taken < 0 ? a.table[(b0 + i) * a.table_stride + slot]
-                                               : a.ring[(uint32_t)(first + take_end[i] - (need[i] - held[i]) + taken) % pages];
+                const uint32_t from = take_end[i] - (uint32_t)(need[i] - held[i]);
+                const int32_t page = taken < 0 ? a.table[(b0 + i) * a.table_stride + slot] : a.ring[in_ring(first + from + (uint32_t)taken)];
                 a.slots[t] = (int64_t)page * a.page_size + (p - slot * a.page_size);
             }
         }
@@ -171,8 +189,8 @@ __global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a, bool table
 
     // ---- what belongs to no sequence, and the whole step's numbers ----------------------
     if (tables) {
-        const Range rest = share(a.rows, done ? all.fresh : 0, a.rows);
-        for (int64_t t = (int64_t)rest.first + tid; t < rest.last; t += kThreads) {
+        const Range rest = share((uint32_t)a.rows, done ? all.fresh : 0, (uint32_t)a.rows);
+        for (uint32_t t = rest.first + tid; t < rest.last; t += T) {
             if (a.pos) a.pos[t] = 0;
             if (a.slots) a.slots[t] = -1;
         }
@@ -182,23 +200,28 @@ __global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a, bool table
         }
     }
     if (lengths && blockIdx.x == 0 && tid == 0) {
-        const int32_t f = a.state[0], n = a.state[1];
-        a.state_out[0] = done ? (int32_t)((uint32_t)(first + all.take) % pages) : f;
-        a.state_out[1] = done ? (int32_t)(free - all.take + all.give) : n;
+        a.state_out[0] = done ? (int32_t)in_ring(first + all.take) : state0;
+        a.state_out[1] = done ? (int32_t)(free - all.take + all.give) : state1;
     }
 }
 
 }  // namespace
 
-hipError_t launch_pages(const PagesArgs& a, hipStream_t s)
+hipError_t launch_pages(const PagesArgs& args, hipStream_t s)
 {
+    PagesArgs a = args;
+    a.by_page = divisor((uint32_t)a.page_size);
     const int64_t groups = std::max((int64_t)1, std::min((int64_t)256, (a.rows + 16 * (int64_t)a.seqs + 4095) / 4096));
     const bool apart = groups > 1 && (a.kv_out == a.kv_len || a.state_out == a.state);
-    hipLaunchKernelGGL(pages_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, a, true, !apart);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !apart) return e;
-    hipLaunchKernelGGL(pages_kernel, dim3(1), dim3(kThreads), 0, s, a, false, true);
-    return hipGetLastError();
+    auto launch = [&](auto kernel, int threads, unsigned n, bool tables, bool lengths) {
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), 0, s, a, tables, lengths);
+        return hipGetLastError();
+    };
+    auto step = [&](unsigned n, bool tables, bool lengths) {
+        return a.seqs <= 256 ? launch(pages_kernel<256>, 256, n, tables, lengths) : launch(pages_kernel<1024>, 1024, n, tables, lengths);
+    };
+    const hipError_t e = step((unsigned)groups, true, !apart);
+    return e != hipSuccess || !apart ? e : step(1, false, true);
 }
 
 }  // namespace tr

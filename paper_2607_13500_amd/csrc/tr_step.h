@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "tr.h"
+#include "tr_divide.h"
 
 namespace tr {
 
@@ -19,6 +20,7 @@ struct PagesArgs {
     int32_t table_width;
     int64_t table_stride;
     int32_t page_size;
+    Divisor by_page;           // filled in by the launch
     int32_t pages;
     int32_t* ring;             // [pages]
     const int32_t* state;      // [2]
@@ -51,7 +53,7 @@ struct VerifyArgs {
 };
 
 // Slices of a row that are summed up one by one.
-constexpr int kSlices = 64;
+constexpr int kSlices = 256;
 
 hipError_t launch_verify(const VerifyArgs& a, bool bf16, hipStream_t s);
 

@@ -95,8 +95,8 @@ tr_status tr_verify_drafts(int64_t T, int32_t vocab, int32_t dtype, const void* 
         return fail(TR_EUNSUPPORTED, "target and draft must be aligned to the element size (%d bytes)", elem_bytes(dtype));
     const uintptr_t words = (uintptr_t)ids | (uintptr_t)q_start | (uintptr_t)accept | (uintptr_t)draw | (uintptr_t)tokens |
                             (uintptr_t)accepted | (uintptr_t)change;
-    if ((words & 3u) || ((uintptr_t)scratch & 7u))
-        return fail(TR_EUNSUPPORTED, "int32 and float arrays must be 4-byte and scratch 8-byte aligned");
+    if ((words & 3u) || ((uintptr_t)scratch & 15u))
+        return fail(TR_EUNSUPPORTED, "int32 and float arrays must be 4-byte and scratch 16-byte aligned");
     tr::VerifyArgs a{};
     a.rows = T;
     a.vocab = vocab;
