@@ -149,118 +149,11 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(RotateArgs g, int parts
     }
 }
 
-// Stores that nothing near reads again: past what the caches hold they are
-// streamed (36864 tokens of 40 bf16 heads of 128 180 -> 170 us, 8 prompts
-// appended 45 -> 38 us).
-template <bool STREAM, typename E>
-__device__ __forceinline__ void put(E* p, Raw<E> v)
-{
-    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<Raw<E>*>(p));
-    else *reinterpret_cast<Raw<E>*>(p) = v;
-}
-
-// Wavefront `first` and those after it: each takes `per` rounds of one token, a
-// round being 64 / LP heads of one side: queries, keys, then values.  A head's address is the round's (the
-// wavefront's) and 32 bits of a lane's.
+// Wavefront `first` and those after it (rotate_wave).
 template <typename E, int LP, bool ADJ, bool APPEND, bool STREAM>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs g, int per, int chunks, uint32_t first)
 {
-    constexpr int R = 64 / LP, DEPTH = 2;
-    const int lane = threadIdx.x & 63, j = lane & (LP - 1), hl = lane / LP;
-    const uint32_t u = first + blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t t = u / (uint32_t)chunks;
-    if (t >= g.tokens) return;
-    const int n0 = (g.heads[0] + R - 1) / R, n1 = n0 + (g.heads[1] + R - 1) / R, all = n1 + (g.heads[2] + R - 1) / R;
-    const int begin = (int)(u - t * (uint32_t)chunks) * per, end = min(all, begin + per);   // the wavefront's rounds
-    const Spot sp = spot_of<ADJ>(j, g.dim, g.rot);
-
-    Raw<E> x0[DEPTH], x1[DEPTH];
-    auto fetch = [&](int d, int i) {
-        if (i >= end) return;
-        const int kind = i < n0 ? 0 : i < n1 ? 1 : 2;
-        const int h = (i - (kind == 0 ? 0 : kind == 1 ? n0 : n1)) * R;
-        const tr_heads in = g.in[kind];
-        if (h + hl < g.heads[kind] && sp.on) {
-            const char* p = static_cast<const char*>(in.p) + ((int64_t)t * in.token + (int64_t)h * in.head) * (int)sizeof(E);
-            const uint32_t at = (uint32_t)hl * ((uint32_t)in.head * (uint32_t)sizeof(E));
-            x0[d] = load(reinterpret_cast<const E*>(p + (at + sp.e0 * (uint32_t)sizeof(E))));
-            x1[d] = load(reinterpret_cast<const E*>(p + (at + sp.e1 * (uint32_t)sizeof(E))));
-        }
-    };
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) fetch(d, begin + d);
-    int64_t row = 0;
-    if constexpr (APPEND) {
-        row = cache_row(g.step, g.cache, t, lane);
-        if (row == kNoToken) return;
-    }
-    Turn z[kPiece];
-    turns_of(g, spin_of(g, j, sp.turns), t, z);
-    Piece wq, wk;
-    if (g.norm) {
-        wq = load_weight<E, ADJ>(g.w[0], sp);
-        wk = load_weight<E, ADJ>(g.w[1], sp);
-    }
-    const float mean = 1.f / (float)g.dim;
-    for (int i0 = begin; i0 < end; i0 += DEPTH) {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int i = i0 + d;
-            if (i >= end) break;
-            const int kind = i < n0 ? 0 : i < n1 ? 1 : 2;
-            const int h = (i - (kind == 0 ? 0 : kind == 1 ? n0 : n1)) * R;
-            const bool live = h + hl < g.heads[kind] && sp.on;
-            Raw<E> y0 = x0[d], y1 = x1[d];
-            fetch(d, i + DEPTH);
-            if (!APPEND || kind < 2) {
-                Piece x = unpack<E, ADJ>(y0, y1);
-                if (g.norm) {
-                    float q = 0.f;
-#pragma unroll
-                    for (int e = 0; e < kPiece; ++e) q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
-                    q = group_sum<LP>(live ? q : 0.f);
-                    float v = fmaf(q, mean, g.eps);
-                    if (__any(live && !in_range(v))) {
-                        const float f = scale_for(v);
-                        q = 0.f;
-#pragma unroll
-                        for (int e = 0; e < kPiece; ++e) {
-                            x.a[e] *= f;
-                            x.b[e] *= f;
-                            q = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], q));
-                        }
-                        v = fmaf(group_sum<LP>(live ? q : 0.f), mean, g.eps * f * f);
-                    }
-                    const float m = rsqrt_(v);
-                    const Piece& w = kind ? wk : wq;
-#pragma unroll
-                    for (int e = 0; e < kPiece; ++e) {
-                        x.a[e] = x.a[e] * m * w.a[e];
-                        x.b[e] = x.b[e] * m * w.b[e];
-                    }
-                }
-                Piece y = x;
-                if (sp.turns) {
-#pragma unroll
-                    for (int e = 0; e < kPiece; ++e) {
-                        y.a[e] = fmaf(x.a[e], z[e].c, -(x.b[e] * z[e].s));
-                        y.b[e] = fmaf(x.b[e], z[e].c, x.a[e] * z[e].s);
-                    }
-                }
-                pack<E, ADJ>(y, y0, y1);
-            }
-            const bool to_cache = APPEND && kind > 0;
-            if (to_cache && row == kNoRow) continue;
-            const int64_t step = to_cache ? g.cache.head : g.out[kind].head;
-            char* p = static_cast<char*>(to_cache ? (kind == 1 ? g.cache.k : g.cache.v) : g.out[kind].p) +
-                      ((to_cache ? row : (int64_t)t * g.out[kind].token) + (int64_t)h * step) * (int)sizeof(E);
-            const uint32_t at = (uint32_t)hl * ((uint32_t)step * (uint32_t)sizeof(E));
-            if (live) {
-                put<STREAM>(reinterpret_cast<E*>(p + (at + sp.e0 * (uint32_t)sizeof(E))), y0);
-                put<STREAM>(reinterpret_cast<E*>(p + (at + sp.e1 * (uint32_t)sizeof(E))), y1);
-            }
-        }
-    }
+    rotate_wave<E, LP, ADJ, APPEND, STREAM>(g, per, chunks, first + blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
 // Gradients of one side (blockIdx.y): a wavefront walks over tokens t, t +
