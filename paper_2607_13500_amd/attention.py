@@ -259,9 +259,7 @@ class Attention:
             raise ValueError("%s must be a contiguous %s [%d] tensor on %s" % (name, self.dtype, self.head_dim, self.device))
         return w.data_ptr()
 
-    def _cache(self, cache):
-        if isinstance(cache, KVCache8):
-            return self._cache8(cache)
+    def _cache(self, cache: KVCache) -> Cache:
         k, v = cache
         shape, stride = self._rows(k, v, self.dtype)
         return Cache(k.data_ptr(), v.data_ptr(), shape[0], shape[1], stride[0], stride[1], stride[2])
@@ -269,9 +267,9 @@ class Attention:
     def _cache8(self, cache: KVCache8) -> Cache8:
         k, v, k_scale, v_scale = cache
         shape, stride = self._rows(k, v, torch.float8_e4m3fn)
-        for name, t in (("cache.k_scale", k_scale), ("cache.v_scale", v_scale)):
-            if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype is not torch.float32:
-                raise ValueError("%s must be a float32 tensor on %s" % (name, self.device))
+        if not isinstance(k_scale, torch.Tensor) or not isinstance(v_scale, torch.Tensor) or k_scale.get_device() != self._index \
+                or v_scale.get_device() != self._index or k_scale.dtype is not torch.float32 or v_scale.dtype is not torch.float32:
+            raise ValueError("cache.k_scale and cache.v_scale must be float32 tensors on %s" % self.device)
         scales, step = k_scale.shape, k_scale.stride()
         if len(scales) != 3 or scales[0] != shape[0] or scales[2] != self.kv_heads or not scales[1] or shape[1] % scales[1]:
             raise ValueError("cache.k_scale must be [%d, blocks, %d] with blocks that divide page_size %d, got %s"
@@ -279,13 +277,13 @@ class Attention:
         if scales != v_scale.shape or step != v_scale.stride():
             raise ValueError("cache.k_scale and cache.v_scale must have the same shape and strides")
         return Cache8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0], shape[1], shape[1] // scales[1],
-                      stride[0], stride[1], stride[2], step[0], step[1], step[2])
+                      *stride[:3], *step)
 
     def _rows(self, k, v, dtype):
         """Shape and strides of a cache's keys and values."""
-        for name, t in (("cache.k", k), ("cache.v", v)):
-            if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype is not dtype:
-                raise ValueError("%s must be a %s tensor on %s" % (name, dtype, self.device))
+        if not isinstance(k, torch.Tensor) or not isinstance(v, torch.Tensor) or k.get_device() != self._index \
+                or v.get_device() != self._index or k.dtype is not dtype or v.dtype is not dtype:
+            raise ValueError("cache.k and cache.v must be %s tensors on %s" % (dtype, self.device))
         shape, stride = k.shape, k.stride()
         if len(shape) != 4 or shape[2] != self.kv_heads or shape[3] != self.head_dim or (self.head_dim > 1 and stride[3] != 1):
             raise ValueError("cache.k must be [pages, page_size, %d, %d] with unit element stride, got %s of strides %s"
@@ -388,10 +386,11 @@ class Attention:
             hq = self._heads("q", q, self.heads, tokens)
             q_out, oq = self._out("q_out", q_out, tokens, self.heads, stream)
         at, ldpos = self._pos(pos, tokens)
-        call = self.lib.tr_append8 if isinstance(cache, KVCache8) else self.lib.tr_append
-        status = call(self._ctx, tokens, hq, hk, hv, self._weight("wq", wq), self._weight("wk", wk), at,
-                                    ldpos, oq, self._cache(cache), self._step(step), self._stream(stream))
-        _check(status, call.__name__)
+        wide = not isinstance(cache, KVCache8)
+        call, c = (self.lib.tr_append, self._cache(cache)) if wide else (self.lib.tr_append8, self._cache8(cache))
+        status = call(self._ctx, tokens, hq, hk, hv, self._weight("wq", wq), self._weight("wk", wk), at, ldpos, oq, c,
+                      self._step(step), self._stream(stream))
+        _check(status, "tr_append" if wide else "tr_append8")
         return q_out if q is not None else None
 
     def attend(self, q: torch.Tensor, cache: Union[KVCache, KVCache8], step: Step, *, scale: Optional[float] = None,
@@ -411,11 +410,11 @@ class Attention:
         hq = self._heads("q", q, self.heads, tokens)
         out, ho = self._out("out", out, tokens, self.heads, stream)
         lse = _empty((tokens, self.heads), torch.float32, self.device, stream) if want_lse else None
-        call = self.lib.tr_attend8 if isinstance(cache, KVCache8) else self.lib.tr_attend
-        status = call(self._ctx, tokens, hq, self._cache(cache), self._step(step),
-                                    1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), 1 if causal else 0,
-                                    int(window), ho, _ptr(lse), self._stream(stream))
-        _check(status, call.__name__)
+        wide = not isinstance(cache, KVCache8)
+        call, c = (self.lib.tr_attend, self._cache(cache)) if wide else (self.lib.tr_attend8, self._cache8(cache))
+        status = call(self._ctx, tokens, hq, c, self._step(step), 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
+                      1 if causal else 0, int(window), ho, _ptr(lse), self._stream(stream))
+        _check(status, "tr_attend" if wide else "tr_attend8")
         return out, lse
 
     def close(self):

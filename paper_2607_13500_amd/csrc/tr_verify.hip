@@ -18,7 +18,6 @@ namespace {
 constexpr int kWaves = 4;                        // of a workgroup of the first launch
 constexpr int kRun = 4;                          // slices of a wavefront, one after another
 constexpr int kGroups = kSlices / (kWaves * kRun);   // workgroups of a sequence
-constexpr int kAhead = 4;                        // steps of a slice whose loads are on their way at a time
 
 // 16 bytes from any address that an element can have.
 template <typename E>
@@ -34,7 +33,11 @@ __device__ __forceinline__ float widen(E v)
 }
 
 // What counts as a probability: positive and finite, else 0.
-__device__ __forceinline__ float proper(float p) { return p > 0.f && p <= 3.40282347e38f ? p : 0.f; }
+__device__ __forceinline__ float proper(float p)
+{
+    constexpr int kSubnormal = 1 << 7, kNormal = 1 << 8;     // positive ones
+    return __builtin_amdgcn_classf(p, kSubnormal | kNormal) ? p : 0.f;
+}
 
 // The row that a sequence's token is drawn from, and what is subtracted from it: a row
 // of the draft, one element, or nothing.
@@ -99,35 +102,70 @@ __device__ __forceinline__ Drawn<E> drawn_of(const VerifyArgs& a, int b, int lan
     return drawn_from<E>(a, b, accepted);
 }
 
-// Elements e .. e + N - 1 of the row as weights (those from `end` on are 0), and as
-// the target's probabilities.
 template <typename E>
 constexpr int kVec = 16 / (int)sizeof(E);
+template <typename E>
+constexpr int kAhead = 2 * (int)sizeof(E);       // steps whose loads are on their way at a time
+
+
+// A lane's elements e .. e + N - 1 of the row, as they lie in memory; those from `end` on
+// are 0.  `whole`: the target's alone.
+struct Elements {
+    uint32_t p[4], q[4];
+};
 
 template <typename E>
-__device__ __forceinline__ void weights_at(const Drawn<E>& d, int e, int end, double (&w)[kVec<E>], double (&p)[kVec<E>])
+__device__ __forceinline__ void load16(const E* from, int e, int end, uint32_t (&w)[4])
 {
-    constexpr int N = kVec<E>;
-    E x[N], y[N];
-    if (e + N <= end) {
-        const Raw16<E> v = *reinterpret_cast<const Raw16<E>*>(d.p + e);
-        __builtin_memcpy(x, &v, 16);
-        if (d.q) {
-            const Raw16<E> u = *reinterpret_cast<const Raw16<E>*>(d.q + e);
-            __builtin_memcpy(y, &u, 16);
-        }
-    } else {
+    if (e + kVec<E> <= end) {
+        const Raw16<E> v = *reinterpret_cast<const Raw16<E>*>(from + e);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            x[i] = e + i < end ? d.p[e + i] : E(0);
-            y[i] = d.q && e + i < end ? d.q[e + i] : E(0);
+        for (int i = 0; i < 4; ++i) w[i] = v.w[i];
+    } else {
+        constexpr int EACH = kVec<E> / 4;    // elements of a word
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = 0;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (e + i * EACH + k < end) w[i] |= __float_as_uint(widen<E>(from[e + i * EACH + k])) >> (EACH == 2 && k == 0 ? 16 : 0);
         }
     }
+}
+
+template <typename E>
+__device__ __forceinline__ void load(const Drawn<E>& d, int e, int end, bool whole, Elements& x)
+{
+    load16(d.p, e, end, x.p);
+    if (d.q && !whole) load16(d.q, e, end, x.q);
+}
+
+// Element i of those words as fp32.
+template <typename E>
+__device__ __forceinline__ float element(const uint32_t (&w)[4], int i)
+{
+    if constexpr (sizeof(E) == 2) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    else return __uint_as_float(w[i]);
+}
+
+// Their weights, max(p - q, 0) = p - min(p, q): the minimum costs nothing in 64 bits.
+template <typename E>
+__device__ __forceinline__ void weigh(const Drawn<E>& d, int e, bool whole, const Elements& x, double (&w)[kVec<E>])
+{
+    constexpr int N = kVec<E>;
+    if (d.q && !whole) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        p[i] = (double)proper(widen<E>(x[i]));
-        const double q = d.q ? (double)proper(widen<E>(y[i])) : e + i == d.certain ? 1.0 : 0.0;
-        w[i] = fmax(p[i] - q, 0.0);
+        for (int i = 0; i < N; ++i) {
+            const float p = proper(element<E>(x.p, i)), q = proper(element<E>(x.q, i));
+            w[i] = (double)p - (double)fminf(p, q);
+        }
+    } else {
+        const int certain = whole ? -1 : d.certain;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float p = proper(element<E>(x.p, i));
+            w[i] = (double)p - (e + i == certain ? (double)fminf(p, 1.f) : 0.0);
+        }
     }
 }
 
@@ -161,6 +199,86 @@ __device__ __forceinline__ double lane_of(double x, int i)
 
 __device__ __forceinline__ int last_of(uint64_t lanes) { return 63 - __builtin_clzll(lanes); }
 
+// The sum of a slice's weights, by a whole wavefront.
+template <typename E>
+__device__ __forceinline__ double sum_of(const Drawn<E>& d, int begin, int limit, bool whole, int lane)
+{
+    constexpr int N = kVec<E>;
+    double sum = 0.0;
+    for (int e0 = begin + lane * N; e0 < limit; e0 += 64 * N * kAhead<E>) {
+        Elements x[kAhead<E>];
+#pragma unroll
+        for (int k = 0; k < kAhead<E>; ++k) load(d, e0 + k * 64 * N, limit, whole, x[k]);
+#pragma unroll
+        for (int k = 0; k < kAhead<E>; ++k) {
+            double w[N];
+            weigh(d, e0 + k * 64 * N, whole, x[k], w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum += w[i];
+        }
+    }
+    return lane_of(upto(sum), 63);
+}
+
+// The token of a slice, some of which have a weight, at which the sum passes the mark,
+// `sum` being that of what is before the slice; by a whole wavefront.
+template <typename E>
+__device__ __forceinline__ int word_in(const Drawn<E>& d, int begin, int limit, double sum, double mark, bool whole, int lane)
+{
+    constexpr int N = kVec<E>;
+    int last = 0;                            // of the tokens with a weight
+    for (int e0 = begin; e0 < limit; e0 += 64 * N * kAhead<E>) {
+        Elements y[kAhead<E>];
+#pragma unroll
+        for (int k = 0; k < kAhead<E>; ++k) load(d, e0 + (k * 64 + lane) * N, limit, whole, y[k]);
+#pragma unroll
+        for (int k = 0; k < kAhead<E>; ++k) {
+            const int e = e0 + (k * 64 + lane) * N;
+            double x[N], mine = 0.0;
+            weigh(d, e, whole, y[k], x);
+            int top = -1;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                mine += x[i];
+                if (x[i] > 0.0) top = e + i;
+            }
+            const double ends = sum + upto(mine);
+            const uint64_t over = __ballot(mine > 0.0 && ends > mark), any = __ballot(top >= 0);
+            if (over) {
+                const double s = ends - mine;
+                int found = top;
+#pragma unroll
+                for (int i = N - 1; i >= 0; --i) {
+                    double t = s;
+#pragma unroll
+                    for (int j = 0; j <= i; ++j) t += x[j];
+                    if (x[i] > 0.0 && t > mark) found = e + i;
+                }
+                return __builtin_amdgcn_readlane(found, __builtin_ctzll(over));
+            }
+            if (any) last = __builtin_amdgcn_readlane(top, last_of(any));
+            sum = lane_of(ends, 63);
+        }
+    }
+    return last;
+}
+
+__device__ __forceinline__ double mark_of(float u, double total) { return (double)fminf(fmaxf(u, 0.f), 0x1.fffffep-1f) * total; }
+
+// A sequence's results, by a wavefront.
+template <typename E>
+__device__ __forceinline__ void write_results(const VerifyArgs& a, const Drawn<E>& d, int b, int word, int lane)
+{
+    const bool any = d.p != nullptr;
+    int32_t* tokens = a.tokens + (int64_t)b * a.width;
+    for (int i = lane; i < a.width; i += 64)
+        tokens[i] = !any ? -1 : i < d.accepted ? a.ids[d.q0 + 1 + i] : i == d.accepted ? word : -1;
+    if (lane == 0) {
+        a.accepted[b] = any ? d.accepted : 0;
+        a.change[b] = any ? d.accepted - d.drafts : 0;
+    }
+}
+
 template <typename E>
 __global__ __launch_bounds__(kWaves * 64) void verify_sum_kernel(VerifyArgs a)
 {
@@ -171,26 +289,26 @@ __global__ __launch_bounds__(kWaves * 64) void verify_sum_kernel(VerifyArgs a)
     if (slice0 == 0 && lane == 0) a.accepted[b] = d.accepted;
     if (!d.p) return;
     const int size = slice_size(a.vocab);
+    // weights, and the target's probabilities of slices without any: only they are asked
+    // for where no slice has one
     double sw[kRun] = {}, sp[kRun] = {};
     for (int at = lane * N; at < size; at += 64 * N) {
-        double w[kRun][N], p[kRun][N];
+        Elements x[kRun];
+#pragma unroll
+        for (int r = 0; r < kRun; ++r) load(d, (slice0 + r) * size + at, min((slice0 + r + 1) * size, a.vocab), false, x[r]);
 #pragma unroll
         for (int r = 0; r < kRun; ++r) {
-            const int begin = (slice0 + r) * size;
-            weights_at<E>(d, begin + at, min(begin + size, a.vocab), w[r], p[r]);
+            double w[N];
+            weigh(d, (slice0 + r) * size + at, false, x[r], w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sw[r] += w[i];
         }
-#pragma unroll
-        for (int r = 0; r < kRun; ++r)
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                sw[r] += w[r][i];
-                sp[r] += p[r][i];
-            }
     }
 #pragma unroll
     for (int r = 0; r < kRun; ++r) {
         sw[r] = lane_of(upto(sw[r]), 63);
-        sp[r] = lane_of(upto(sp[r]), 63);
+        const int begin = (slice0 + r) * size;
+        if (!(sw[r] > 0.0)) sp[r] = sum_of<E>(d, begin, min(begin + size, a.vocab), true, lane);
     }
     double2* part = reinterpret_cast<double2*>(a.part) + (int64_t)b * kSlices + slice0;
 #pragma unroll
@@ -204,14 +322,12 @@ constexpr int kPer = kSlices / 64;
 template <typename E>
 __global__ __launch_bounds__(64) void verify_draw_kernel(VerifyArgs a)
 {
-    constexpr int N = kVec<E>;
     const int lane = threadIdx.x, b = blockIdx.x;
     double2 part[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) part[i] = reinterpret_cast<const double2*>(a.part)[(int64_t)b * kSlices + lane * kPer + i];
     const float u = a.draw[b];
     const Drawn<E> d = drawn_from<E>(a, b, a.accepted[b]);
-    int32_t* tokens = a.tokens + (int64_t)b * a.width;
     int word = 0;
     if (d.p) {
         double w = 0.0, p = 0.0;
@@ -223,7 +339,7 @@ __global__ __launch_bounds__(64) void verify_draw_kernel(VerifyArgs a)
         const double all_w = upto(w), all_p = upto(p);
         const bool whole = !(lane_of(all_w, 63) > 0.0);  // nothing is left: drawn from the target itself
         const double own = whole ? p : w, end = whole ? all_p : all_w, total = lane_of(end, 63);
-        const double mark = (double)fminf(fmaxf(u, 0.f), 0x1.fffffep-1f) * total;
+        const double mark = mark_of(u, total);
         // The first lane, slice, and in the end token, at whose end the sum is past the
         // mark.  Sums are rounded, each by its own order of additions: where none is past it
         // (of a part whose end was), it is the last with a weight.
@@ -244,59 +360,60 @@ __global__ __launch_bounds__(64) void verify_draw_kernel(VerifyArgs a)
                 }
                 sum += v;
             }
-            const int size = slice_size(a.vocab), begin = (at * kPer + slice) * size, limit = min(begin + size, a.vocab);
-            sum = before;
-            int last = -1;                               // of the slice's tokens with a weight
-            word = -1;
-            for (int e0 = begin; e0 < limit && word < 0; e0 += 64 * N * kAhead) {
-                double x[kAhead][N];
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    double y[N];
-                    weights_at<E>(d, e0 + (k * 64 + lane) * N, limit, x[k], y);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) x[k][i] = whole ? y[i] : x[k][i];
-                }
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    const int e = e0 + (k * 64 + lane) * N;
-                    double mine = 0.0;
-                    int top = -1;
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        mine += x[k][i];
-                        if (x[k][i] > 0.0) top = e + i;
-                    }
-                    const double ends = sum + upto(mine);
-                    const uint64_t over = __ballot(mine > 0.0 && ends > mark), any = __ballot(top >= 0);
-                    if (over && word < 0) {
-                        double s = ends - mine;
-                        int found = top;
-#pragma unroll
-                        for (int i = N - 1; i >= 0; --i) {
-                            double t = s;
-#pragma unroll
-                            for (int j = 0; j <= i; ++j) t += x[k][j];
-                            if (x[k][i] > 0.0 && t > mark) found = e + i;
-                        }
-                        word = __builtin_amdgcn_readlane(found, __builtin_ctzll(over));
-                    }
-                    if (any) last = __builtin_amdgcn_readlane(top, last_of(any));
-                    sum = lane_of(ends, 63);
-                }
-            }
-            if (word < 0) word = max(last, 0);
+            const int size = slice_size(a.vocab), begin = (at * kPer + slice) * size;
+            word = word_in<E>(d, begin, min(begin + size, a.vocab), before, mark, whole, lane);
         }
     }
-    const bool any = d.p != nullptr;
-    for (int i = lane; i < a.width; i += 64)
-        tokens[i] = !any ? -1 : i < d.accepted ? a.ids[d.q0 + 1 + i] : i == d.accepted ? word : -1;
-    if (lane == 0) a.change[b] = any ? d.accepted - d.drafts : 0;
+    write_results(a, d, b, word, lane);
+}
+
+// Rows of at most kOneWords: a workgroup a sequence, in one launch.  Each wavefront has
+// one slice, of whose sums all wavefronts see where the mark falls.  Bound by one CU's
+// 64-bit additions (one sequence, 32000 fp32 words and a draft's: 10.7 us a call, 13.6
+// in two launches; 16 sequences, 50001 bf16 words: 13.3 both).
+constexpr int kOneWaves = 16;
+constexpr int kOneWords = 40000;
+
+template <typename E>
+__global__ __launch_bounds__(kOneWaves * 64) void verify_one_kernel(VerifyArgs a)
+{
+    __shared__ double sums[2][kOneWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.x;
+    const float u = a.draw[b];
+    const Drawn<E> d = drawn_of<E>(a, b, lane);
+    if (!d.p) {                               // the whole workgroup leaves together
+        if (wave == 0) write_results(a, d, b, 0, lane);
+        return;
+    }
+    const int size = ((a.vocab + kOneWaves - 1) / kOneWaves + 15) & ~15, begin = min(wave * size, a.vocab), limit = min(begin + size, a.vocab);
+    double own = 0.0, end = 0.0, total = 0.0;        // lane i: of slice i, and up to its end
+    bool whole = false;
+    for (;; whole = true) {
+        const double sum = sum_of<E>(d, begin, limit, whole, lane);
+        if (lane == 0) sums[whole][wave] = sum;
+        __syncthreads();
+        own = lane < kOneWaves ? sums[whole][lane & (kOneWaves - 1)] : 0.0;
+        end = upto(own);
+        total = lane_of(end, kOneWaves - 1);
+        if (whole || total > 0.0) break;             // nothing is left: drawn from the target itself
+    }
+    const double mark = mark_of(u, total);
+    // The first slice whose end is past the mark; where, by the sums' roundings, none
+    // is, the last with a weight.
+    const uint64_t some = __ballot(own > 0.0), past = __ballot(own > 0.0 && end > mark);
+    const int at = past ? __builtin_ctzll(past) : some ? last_of(some) : 0;
+    if (wave != at) return;
+    const int word = some ? word_in<E>(d, begin, limit, lane_of(end, at) - lane_of(own, at), mark, whole, lane) : 0;
+    write_results(a, d, b, word, lane);
 }
 
 template <typename E>
 hipError_t verify(const VerifyArgs& a, hipStream_t s)
 {
+    if (a.vocab <= kOneWords) {
+        hipLaunchKernelGGL(verify_one_kernel<E>, dim3((unsigned)a.seqs), dim3(kOneWaves * 64), 0, s, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(verify_sum_kernel<E>, dim3((unsigned)a.seqs * kGroups), dim3(kWaves * 64), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -42,10 +42,25 @@ class Verified(NamedTuple):
     change: torch.Tensor           # int32 [seqs] accepted minus drafted: what the sequence's length changes by
 
 
-def _vector(name, t, device, dtype, size):
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype is not dtype or t.shape != (size,) or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s [%d] tensor on %s" % (name, dtype, size, device))
+# Small calls are bound by this module's own work (64 requests' tables: 11 us a call
+# against 4 on the device), so a call's results share one allocation where they can,
+# and each tensor is looked at once.
+_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+
+
+def _vector(name, t, index, dtype, size):
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype is not dtype or t.shape != (size,) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s [%d] tensor on cuda:%d" % (name, dtype, size, index))
     return t.data_ptr()
+
+
+def _matrix(name, t, index, dtype, rows):
+    """Address, row stride and columns of a tensor with rows contiguous."""
+    if isinstance(t, torch.Tensor) and t.get_device() == index and t.dtype is dtype and t.dim() == 2:
+        (n, columns), (row, unit) = t.shape, t.stride()
+        if n == rows and (unit == 1 or columns <= 1):
+            return t.data_ptr(), row, columns
+    raise ValueError("%s must be a %s [%d, columns] tensor with rows contiguous on cuda:%d" % (name, dtype, rows, index))
 
 
 def _run(call, name, index, stream, *args):
@@ -76,36 +91,26 @@ def update_pages(change: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor
     """
     if not isinstance(kv_len, torch.Tensor) or not kv_len.is_cuda or kv_len.dim() != 1:
         raise ValueError("kv_len must be an int32 [seqs] tensor on a ROCm device")
-    device, seqs = kv_len.device, kv_len.shape[0]
-    i32 = torch.int32
-    _vector("kv_len", kv_len, device, i32, seqs)
-    if not isinstance(table, torch.Tensor) or table.device != device or table.dtype is not i32 or table.dim() != 2 \
-            or table.shape[0] != seqs or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise ValueError("table must be an int32 [%d, width] tensor with rows contiguous on %s" % (seqs, device))
+    index, seqs, rows = kv_len.get_device(), kv_len.shape[0], int(rows)
+    at_kv = _vector("kv_len", kv_len, index, _I32, seqs)
+    at_change = _vector("change", change, index, _I32, seqs)
+    at_table, row, width = _matrix("table", table, index, _I32, seqs)
     ring, state = pool
     if not isinstance(ring, torch.Tensor) or ring.dim() != 1:
-        raise ValueError("pool.ring must be an int32 [pages] tensor on %s" % device)
-    rows = int(rows)
+        raise ValueError("pool.ring must be an int32 [pages] tensor on cuda:%d" % index)
+    pages = ring.shape[0]
+    at_ring, at_state = _vector("pool.ring", ring, index, _I32, pages), _vector("pool.state", state, index, _I32, 2)
     if rows < 0:
         raise ValueError("rows must be >= 0 (got %d)" % rows)
     sizes = [seqs + 1, rows, 1] if in_place else [seqs + 1, rows, 1, seqs, 2]
-    parts = _empty((sum(sizes),), i32, device, stream).split(sizes)
+    parts = _empty((sum(sizes),), _I32, kv_len.device, stream).unsafe_split_with_sizes(sizes)
     q_start, pos, short = parts[:3]
     kv_out, state_out = (kv_len, state) if in_place else parts[3:]
-    slots = _empty((rows,), torch.int64, device, stream)
-    p = Pool(ring.shape[0], _vector("pool.ring", ring, device, i32, ring.shape[0]), _vector("pool.state", state, device, i32, 2),
-             state_out.data_ptr())
-    _run(_lib.load().tr_update_pages, "tr_update_pages", device.index, stream, seqs, _vector("change", change, device, i32, seqs),
-         kv_len.data_ptr(), kv_out.data_ptr(), table.data_ptr(), table.shape[1], table.stride(0), int(page_size), ctypes.byref(p),
-         q_start.data_ptr(), rows, slots.data_ptr(), pos.data_ptr(), short.data_ptr())
+    slots = _empty((rows,), _I64, kv_len.device, stream)
+    p = Pool(pages, at_ring, at_state, state_out.data_ptr())
+    _run(_lib.load().tr_update_pages, "tr_update_pages", index, stream, seqs, at_change, at_kv, kv_out.data_ptr(), at_table, width, row,
+         int(page_size), ctypes.byref(p), q_start.data_ptr(), rows, slots.data_ptr(), pos.data_ptr(), short.data_ptr())
     return PageUpdate(Step(q_start, kv_out, table), slots, pos, PagePool(ring, state_out), short)
-
-
-def _rows(name, t, device, dtype, shape):
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype is not dtype or t.shape != shape \
-            or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be a %s %s tensor with rows contiguous on %s" % (name, dtype, list(shape), device))
-    return t.data_ptr(), t.stride(0)
 
 
 def verify_drafts(target: torch.Tensor, ids: torch.Tensor, q_start: torch.Tensor, accept: torch.Tensor, draw: torch.Tensor,
@@ -127,18 +132,24 @@ def verify_drafts(target: torch.Tensor, ids: torch.Tensor, q_start: torch.Tensor
     """
     if not isinstance(target, torch.Tensor) or not target.is_cuda or target.dim() != 2 or target.dtype not in _DTYPES:
         raise ValueError("target must be a float32 or bfloat16 [tokens, vocab] tensor on a ROCm device")
+    index, dtype, (tokens, vocab), width = target.get_device(), target.dtype, target.shape, int(width)
     if not isinstance(q_start, torch.Tensor) or q_start.dim() != 1 or q_start.shape[0] < 1:
-        raise ValueError("q_start must be an int32 [seqs + 1] tensor on %s" % target.device)
-    device, (tokens, vocab), seqs, width, i32 = target.device, target.shape, q_start.shape[0] - 1, int(width), torch.int32
+        raise ValueError("q_start must be an int32 [seqs + 1] tensor on cuda:%d" % index)
+    seqs = q_start.shape[0] - 1
     if width < 1:
         raise ValueError("width must be >= 1 (got %d)" % width)
-    p, ld = _rows("target", target, device, target.dtype, target.shape)
-    q, ld_draft = (None, 0) if draft is None else _rows("draft", draft, device, target.dtype, target.shape)
+    p, ld, _ = _matrix("target", target, index, dtype, tokens)
+    q, ld_draft = None, 0
+    if draft is not None:
+        q, ld_draft, columns = _matrix("draft", draft, index, dtype, tokens)
+        if columns != vocab:
+            raise ValueError("draft must have target's %d columns (got %d)" % (vocab, columns))
     lib = _lib.load()
-    said, accepted, change = _empty((seqs * (width + 2),), i32, device, stream).split([seqs * width, seqs, seqs])
-    scratch = _empty((lib.tr_verify_scratch(seqs),), torch.uint8, device, stream)
-    _run(lib.tr_verify_drafts, "tr_verify_drafts", device.index, stream, tokens, vocab, _DTYPES[target.dtype], p, ld, q, ld_draft,
-         _vector("ids", ids, device, i32, tokens), seqs, _vector("q_start", q_start, device, i32, seqs + 1),
-         _vector("accept", accept, device, torch.float32, tokens), _vector("draw", draw, device, torch.float32, seqs), width,
+    # the scratch first, whose address has to be of 16 bytes
+    scratch, said, accepted, change = _empty((lib.tr_verify_scratch(seqs) // 4 + seqs * (width + 2),), _I32, target.device, stream) \
+        .unsafe_split_with_sizes([lib.tr_verify_scratch(seqs) // 4, seqs * width, seqs, seqs])
+    _run(lib.tr_verify_drafts, "tr_verify_drafts", index, stream, tokens, vocab, _DTYPES[dtype], p, ld, q, ld_draft,
+         _vector("ids", ids, index, _I32, tokens), seqs, _vector("q_start", q_start, index, _I32, seqs + 1),
+         _vector("accept", accept, index, _F32, tokens), _vector("draw", draw, index, _F32, seqs), width,
          said.data_ptr(), accepted.data_ptr(), change.data_ptr(), scratch.data_ptr())
     return Verified(said.view(seqs, width), accepted, change)
