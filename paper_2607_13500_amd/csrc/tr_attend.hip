@@ -800,7 +800,7 @@ hipError_t attend(const AttendArgs& args, hipStream_t s)
 
 }  // namespace
 
-size_t attend_groups(int cus) { return (size_t)std::max({kFewPerCu<64>, kFewPerCu<128>, kFewPerCu<256>, 1}) * cus; }
+size_t attend_groups(int cus) { return (size_t)8 * cus; }
 
 size_t attend_part_floats(int dim, int cus)
 {

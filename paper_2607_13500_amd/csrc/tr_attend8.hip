@@ -27,17 +27,17 @@ __device__ __forceinline__ int64_t lane_of(int64_t x, int i)
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, i));
 }
 
-// Eight e4m3 values as bf16, times a power of two.
-__device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float by = 1.f)
+// Eight e4m3 values as bf16, four and four times a power of two.
+__device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float by_a = 1.f, float by_b = 1.f)
 {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     struct {
         bf16x2 v[4];
     } r;
-    r.v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, false);
-    r.v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, true);
-    r.v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, false);
-    r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, true);
+    r.v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by_a, false);
+    r.v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by_a, true);
+    r.v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by_b, false);
+    r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by_b, true);
     return __builtin_bit_cast(bf16x8, r);
 }
 
@@ -53,29 +53,71 @@ __device__ __forceinline__ int piece8(int row, int piece)
     return piece ^ (DH == 64 ? (row >> 1) & 3 : row & 7);
 }
 
+// Whether a scale is a power of two (and a normal number) by which widening is exact.
+__device__ __forceinline__ bool is_power(float s)
+{
+    const uint32_t w = __float_as_uint(s);
+    return (w & 0x807fffffu) == 0 && w - (10u << 23) < (238u << 23);       // 2^-117 .. 2^120
+}
+
+// Queries whose scores are for scale > 0: of -q for scale < 0, of q = 0 for scale 0, NaN
+// where it is not finite.
+__device__ __forceinline__ bf16x8 signed_query(const AttendArgs& a, u32x4 v)
+{
+    if (a.keep == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = ((v[i] & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u);
+    }
+    return __builtin_bit_cast(bf16x8, v ^ a.flip);
+}
+
+// A factor of scores.  Those of keys that no row sees may be anything; 0 would make NaN
+// of -inf, which the smallest normal number does not.
+__device__ __forceinline__ float factor(float x) { return fmaxf(x, 0x1p-126f); }
+
+// The largest over the four groups of 16 lanes.
+__device__ __forceinline__ float max_groups(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    const float y = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[1]));
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+    return max3(__uint_as_float(q[0]), __uint_as_float(q[1]), __uint_as_float(q[1]));
+}
+
 // ---- few rows over many keys -----------------------------------------------------------
-// Items are RT tiles of 16 rows, steps 4 kTile keys; the four wavefronts take tiles of
-// kTile keys in turn, as in the bf16 kernel, and what is widened of a tile serves all its rows.
+// Items are RT tiles of 16 rows, in steps of kStep keys, and what is widened of a tile
+// of keys serves all its rows.  A workgroup's four wavefronts either take tiles of kTile
+// keys of one key head in turn and join their sums at an item's end (HW = 1), or have a key
+// head each (HW = 4, items then are those of four heads), for heads of 64, whose rows are
+// half a line of memory: read at the same time side by side they come faster (32
+// requests with 2 to 8 tokens each 104 us instead of 148; 64 requests with one 139
+// instead of 211; heads of 128 are no faster so).
+//
+// Bound by the bytes of the cache, in calls of single tokens by the latency of what
+// waits for one another (lengths, table, keys, the join of parts).  A wavefront has the
+// next tile's 8 KB on their way into registers while it works on one.  One workgroup
+// of a CU reads as fast as several, and there are fewer parts to join (64 requests
+// over 256 to 16384 tokens, 4 heads of 128: 109 us, 5.65 TB/s; 118 with two, 129 with
+// three; with tiles of 64 keys 119).
 template <int DH>
 constexpr int kFewTile = DH == 64 ? 64 : 32;
 
-template <int DH, int RT>
-constexpr int kFewPerCu8 = DH == 256 ? 1 : RT == 4 ? (DH == 64 ? 2 : 1) : RT == 2 ? 2 : 3;
-
 // PG16: pages and blocks of whole halves of a tile (multiples of 16 tokens, pages below
 // 2 GB), so that a half's page and scales are the wavefront's.  FULL: head_dim is DH.
-template <int DH, int RT, bool PG16, bool FULL>
-__global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few_kernel(Attend8Args a)
+// kv_heads counts groups of HW heads here.
+template <int DH, int HW, int RT, bool PG16, bool FULL>
+__global__ __launch_bounds__(kFewThreads, 1) void attend8_few_kernel(Attend8Args a)
 {
-    constexpr int ROWS = 16 * RT, kTile = kFewTile<DH>, kStep = 4 * kTile;
+    constexpr int ROWS = 16 * RT, kTile = kFewTile<DH>, kStep = 4 / HW * kTile;
     constexpr int X = kTile / 16, C = kTile / 32;      // sixteens of keys and fragments of weights of a tile
     constexpr int KF = DH / 32, DT = DH / 16;          // fragments of keys, tiles of elements
     constexpr int PIECES = DH / 16, VR = 64 / PIECES, VN = kTile / VR;   // pieces of a row, rows of a load, loads of a tile
     constexpr int PAD = DH + 4;
     constexpr int BYTES = kTile * DH;
-    constexpr int kLds = 4 * std::max(2 * BYTES, 16 * PAD * 4);
+    constexpr int kLds = 4 * (HW == 1 ? std::max(2 * BYTES, 16 * PAD * 4) : 2 * BYTES);
     __shared__ __align__(16) unsigned char smem[kLds];
-    __shared__ float ml[4][2][16];
+    [[maybe_unused]] __shared__ float ml[4][2][16];
     __shared__ int flag;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -86,52 +128,30 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
     const int token_bytes = (int)a.cache8.token;                 // PG16
     const uint32_t in_lane = (uint32_t)(vrow * token_bytes + piece * 16);
 
-    const Shares all = shares_of<ROWS, kStep>(a, lane);
+    Place pl;
+    const Shares all = first_place<ROWS, kStep, HW>(a, lane, pl);
     int64_t u = (int64_t)blockIdx.x * all.share;
     const int64_t u_end = min(u + all.share, all.total);
 
-    int from = 0;
-    int64_t before = 0;
-    while (u < u_end) {
-        const Place pl = place_of<ROWS, kStep>(a, u, lane, from, before);
-        from = pl.b;
-        before = pl.first;
+    for (bool first_item = true; u < u_end; first_item = false) {
+        if (!first_item) pl = place_of<ROWS, kStep>(a, u, lane, pl.b, pl.first, all.extra);
         const Sequence s = pl.s;
         const int64_t local = u - pl.first;
-        const int item = (int)(local / pl.steps), step0 = (int)(local - (int64_t)item * pl.steps);
-        const int step1 = (int)min((int64_t)pl.steps, step0 + (u_end - u));
-        const int rt = item / a.kv_heads, h = item - rt * a.kv_heads;
-        const bool whole = step0 == 0 && step1 == pl.steps;
+        const int item = (int)(local / pl.steps), part0 = (int)(local - (int64_t)item * pl.steps);
+        const int part1 = (int)min((int64_t)pl.steps, part0 + (u_end - u));
+        const int step0 = max(0, part0 - all.extra), step1 = max(0, part1 - all.extra);
+        const int rt = item / a.kv_heads, h = (item - rt * a.kv_heads) * HW + wave % HW;
+        const bool whole = part0 == 0 && part1 == pl.steps;
 
-        // ---- this lane's rows, one of each tile ---------------------------------------
-        const int rows = (int)min((int64_t)ROWS, (int64_t)s.n * a.group - (int64_t)rt * ROWS);
+        // ---- the rows' bounds: this lane's, one of each tile, and all rows' -----------
+        const int rows = (int)min((int64_t)ROWS, (int64_t)s.n * a.group - (int64_t)rt * ROWS);     // of each head
         int lo[RT], hi[RT];
-        bf16x8 qf[RT][KF];
-        f32x4 o[RT][DT];
-        float m[RT], l[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const uint32_t r = (uint32_t)(rt * ROWS + 16 * i + col);
-            const int tok = (int)divide(r, a.by_group), head = h * a.group + (int)(r - (uint32_t)tok * a.group);
-            const bool live = 16 * i + col < rows;
             lo[i] = hi[i] = 0;
-            if (live) seen_by(a, s, tok, lo[i], hi[i]);
-            // elements in the order in which widened keys have them: 16 of a lane's group
-            // after another, 8 to a fragment
-#pragma unroll
-            for (int k = 0; k < KF; ++k) {
-                const int e = (k / 2) * 64 + grp * 16 + (k % 2) * 8;
-                u32x4 v{};
-                if (live && e < a.dim)
-                    v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q.p) + (s.q0 + tok) * a.q.token + (int64_t)head * a.q.head + e);
-                qf[i][k] = __builtin_bit_cast(bf16x8, v);
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-            m[i] = minus_inf();
-            l[i] = 0.f;
+            if (16 * i + col < rows) seen_by(a, s, (int)divide((uint32_t)(rt * ROWS + 16 * i + col), a.by_group), lo[i], hi[i]);
         }
-        int lo_min, lo_max, hi_min, hi_max;       // over all rows
+        int lo_min, lo_max, hi_min, hi_max;
         {
             const int t0 = (int)divide((uint32_t)rt * ROWS, a.by_group), t1 = (int)divide((uint32_t)(rt * ROWS + rows - 1), a.by_group);
             seen_by(a, s, t0, lo_min, hi_min);
@@ -141,7 +161,7 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
         // ---- keys -------------------------------------------------------------------
         const int base = s.begin & ~(kAlign - 1);
         const int j_end = min(hi_max, base + step1 * kStep);
-        const int first = base + step0 * kStep + wave * kTile;
+        const int first = base + step0 * kStep + wave / HW * kTile;
         // tiles before any row's range are skipped
         int j0 = first;
         if (j0 + kTile <= lo_min) j0 += ((lo_min - j0) / kStep) * kStep;
@@ -160,9 +180,9 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
         // place of the nearest one.
         // Else a lane looks up a key of one tile, a tile ahead.
         constexpr int BT = 64 / X;
-        int page = 0, in = 0, ahead = 0;          // ahead: tiles that are looked up and not fetched
+        int page = 0, in = 0, ahead = 0, at = 0;  // ahead: tiles that are looked up and not fetched; at: the fetched tile's first lane
         int64_t off = 0;
-        float ks = 0.f, vs = 0.f, ks_next[X], vs_next[X];
+        float ks = 0.f, vs = 0.f;
         auto look = [&](int j) {
             const int t = PG16 ? min(max(j + (lane / X) * kStep + (lane % X) * 16, lo_min & ~15), last & ~15)
                                : min(max(j + (lane & (kTile - 1)), lo_min), last);
@@ -184,13 +204,11 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
                     find();
                     ahead = BT;
                 }
-                const int at = (BT - ahead) * X;
+                at = (BT - ahead) * X;
                 --ahead;
                 constexpr int EACH = VN / X;
 #pragma unroll
                 for (int x = 0; x < X; ++x) {
-                    ks_next[x] = lane_of(ks, at + x);
-                    vs_next[x] = lane_of(vs, at + x);
                     const int64_t o = lane_of(off, at + x);
 #pragma unroll
                     for (int i = 0; i < EACH; ++i) {
@@ -223,6 +241,29 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
             if constexpr (!PG16) look(j0);
             fetch(j0);
         }
+
+        bf16x8 qf[RT][KF];
+        f32x4 o[RT][DT];
+        float m[RT], l[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const uint32_t r = (uint32_t)(rt * ROWS + 16 * i + col);
+            const int tok = (int)divide(r, a.by_group), head = h * a.group + (int)(r - (uint32_t)tok * a.group);
+            // elements in the order in which widened keys have them: 16 of a lane's group
+            // after another, 8 to a fragment
+#pragma unroll
+            for (int k = 0; k < KF; ++k) {
+                const int e = (k / 2) * 64 + grp * 16 + (k % 2) * 8;
+                u32x4 v{};
+                if (16 * i + col < rows && e < a.dim)
+                    v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q.p) + (s.q0 + tok) * a.q.token + (int64_t)head * a.q.head + e);
+                qf[i][k] = signed_query(a, v);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m[i] = minus_inf();
+            l[i] = 0.f;
+        }
         for (; j0 < j_end; j0 += kStep) {
             // rows that see different tokens of this tile: a NaN must not reach the rows
             // that do not see it
@@ -246,11 +287,12 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
                 *reinterpret_cast<u32x4*>(kt + row * DH + piece8<DH>(row, piece) * 16) = kr[i];
                 *reinterpret_cast<u32x4*>(vt + row * DH + piece8<DH>(row, piece) * 16) = vr[i];
             }
+            // the tile's scales: of its sixteens, or of this lane's key
             float ks_tile[X], vs_tile[X];
 #pragma unroll
             for (int x = 0; x < X; ++x) {
-                ks_tile[x] = ks_next[x];
-                vs_tile[x] = vs_next[x];
+                ks_tile[x] = PG16 ? lane_of(ks, at + x) : 0.f;
+                vs_tile[x] = PG16 ? lane_of(vs, at + x) : 0.f;
             }
             const float ks_lane = ks, vs_lane = vs;
             if (j0 + kStep < j_end) fetch(j0 + kStep);
@@ -273,53 +315,91 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
             }
 
             // ---- weights ------------------------------------------------------------
-            float kf[4 * X], vf[4 * X];           // scales of this lane's keys
+            // Factors of the scores, of sixteen keys each (else in the scores already), and
+            // the values' scales: powers of two are for the widening, others for the weights.
+            float f[X];
+            bool folded = PG16;
 #pragma unroll
-            for (int x = 0; x < X; ++x)
+            for (int x = 0; x < X; ++x) {
+                if constexpr (PG16) {
+                    f[x] = factor(ks_tile[x] * a.scale);
+                    folded = folded && is_power(vs_tile[x]);
+                } else {
+                    f[x] = 1.f;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    kf[4 * x + v] = (PG16 ? ks_tile[x] : __shfl(ks_lane, 16 * x + 4 * grp + v)) * a.scale;
-                    vf[4 * x + v] = PG16 ? vs_tile[x] : __shfl(vs_lane, 16 * x + 4 * grp + v);
+                    for (int v = 0; v < 4; ++v) {
+                        const float z = factor(__shfl(ks_lane, 16 * x + 4 * grp + v) * a.scale);
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) sc[i][x][v] *= z;
+                    }
                 }
+            }
+            const bool edge = j0 < lo_max || j0 + kTile > hi_min;     // rows past the last are nobody's
+            // No branch lies between a matrix instruction and a reader of its result, but for
+            // those that skip what all of a tile's rows would do: where several ways lead to a
+            // reader the compiler does not count its wait on all of them.
             u32x4 pb[RT][C];
+            float top[RT];
+            bool left[RT], any = false;
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                // Tiles without rows are left out of the weights, but not of the products: a
-                // branch may not lie between a matrix instruction and a reader of its result,
-                // whose wait the compiler then does not count on every way there.
+                if (edge) {
+                    asm volatile("");      // a branch: most tiles need none of this
 #pragma unroll
-                for (int c = 0; c < C; ++c) pb[i][c] = u32x4{};
-                if (i > 0 && 16 * i >= rows) continue;
-                float p[4 * X];
-                float top = minus_inf();
+                    for (int x = 0; x < X; ++x)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const int j = j0 + 16 * x + 4 * grp + v;
+                            sc[i][x][v] = j >= lo[i] && j < hi[i] ? sc[i][x][v] : minus_inf();
+                        }
+                }
+                top[i] = minus_inf();
+#pragma unroll
+                for (int x = 0; x < X; ++x) {
+                    const f32x4 z = sc[i][x];
+                    const float t = max3(z[0], z[1], max3(z[2], z[3], z[3]));
+                    top[i] = max3(top[i], t * f[x], top[i]);
+                }
+                top[i] = max_groups(top[i]);
+                // The maximum that a row's weights are relative to follows only when it is
+                // left behind by 2^8: sums scaled by less than that lose nothing.
+                left[i] = top[i] - m[i] > 8.f;
+                any = any || left[i];
+            }
+            if (__any(any)) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const float keep = left[i] ? exp2_(m[i] - top[i]) : 1.f;
+                    m[i] = left[i] ? top[i] : m[i];
+                    l[i] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[i][d] *= keep;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const float zero = m[i] == minus_inf() ? 0.f : m[i];
+                float p[4 * X], sum = 0.f;
 #pragma unroll
                 for (int x = 0; x < X; ++x)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const int j = j0 + 16 * x + 4 * grp + v;
-                        const float y = sc[i][x][v] * kf[4 * x + v];
-                        p[4 * x + v] = j >= lo[i] && j < hi[i] ? y : minus_inf();
-                        top = fmaxf(top, p[4 * x + v]);
+                        p[4 * x + v] = exp2_(fmaf(sc[i][x][v], f[x], -zero));
+                        sum += p[4 * x + v];
                     }
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float m1 = fmaxf(m[i], top), zero = m1 == minus_inf() ? 0.f : m1;
-                const bool same = m1 == m[i];             // rows that see nothing yet among them
-                const float keep = exp2_(m[i] - zero);
-                m[i] = m1;
-                l[i] *= keep;
+                l[i] += sum;
+                if (!folded) {
 #pragma unroll
-                for (int v = 0; v < 4 * X; ++v) {
-                    p[v] = exp2_(p[v] - zero);
-                    l[i] += p[v];
-                    p[v] = p[v] == 0.f ? 0.f : p[v] * vf[v];      // a token that is not seen may have any scale
+                    for (int x = 0; x < X; ++x)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            // a token that is not seen may have any scale
+                            const float z = PG16 ? vs_tile[x] : __shfl(vs_lane, 16 * x + 4 * grp + v);
+                            p[4 * x + v] = p[4 * x + v] == 0.f ? 0.f : p[4 * x + v] * z;
+                        }
                 }
 #pragma unroll
                 for (int v = 0; v < 2 * X; ++v) pb[i][v / 4][v % 4] = pack_bf16(p[2 * v], p[2 * v + 1]);
-                if (!__all(same)) {
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[i][d] *= keep;
-                }
             }
             // ---- values ---------------------------------------------------------------
             if (__any(bad)) {
@@ -351,95 +431,182 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
                     const int n = (lane & 15) >> 1, row = 32 * c + 4 * grp + (n & 3) + 16 * (n >> 2);
                     const unsigned char* q = vt + row * DH + piece8<DH>(row, d) * 16 + (lane & 1) * 8;
                     const i32x2 t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)q);
-                    const bf16x8 w = widen8((uint32_t)t.x, (uint32_t)t.y);
+                    const bf16x8 w = widen8((uint32_t)t.x, (uint32_t)t.y, folded ? vs_tile[2 * c] : 1.f, folded ? vs_tile[2 * c + 1] : 1.f);
 #pragma unroll
-                    for (int i = 0; i < RT; ++i) {
+                    for (int i = 0; i < RT; ++i)
                         o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, pb[i][c]), o[i][d], 0, 0, 0);
-                    }
                 }
         }
 
-        // ---- the four wavefronts' parts, a tile of rows after another --------------------
-        constexpr int F = kPartFloats<DH, ROWS>;
-        constexpr int N = DH / 16;                // elements of a thread
-        const int row = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * N;
+        constexpr int F = kPartFloats<DH, ROWS * HW>;
         const int64_t begin = pl.first + (int64_t)item * pl.steps;
         const Parts parts = parts_of(begin, begin + pl.steps, all.share);
-        float* red = reinterpret_cast<float*>(smem);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             l[i] += __shfl_xor(l[i], 16);
             l[i] += __shfl_xor(l[i], 32);
-            __syncthreads();
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-                *reinterpret_cast<f32x4*>(red + (wave * 16 + col) * PAD + 16 * d + 4 * grp) = o[i][d];
-            if (grp == 0) {
-                ml[wave][0][col] = m[i];
-                ml[wave][1][col] = l[i];
-            }
-            __syncthreads();
-            float top = minus_inf();
-#pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][0][row]);
-            const float zero = top == minus_inf() ? 0.f : top;
-            float sum = 0.f, acc[N] = {};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float f = exp2_(ml[w][0][row] - zero);
-                sum = fmaf(ml[w][1][row], f, sum);
-#pragma unroll
-                for (int e = 0; e < N; ++e) acc[e] = fmaf(red[(w * 16 + row) * PAD + e0 + e], f, acc[e]);
-            }
-            const int mine = 16 * i + row;        // of the item's rows
-            if (mine >= rows) continue;
-            if (whole) {
-                const uint32_t r = (uint32_t)(rt * ROWS + mine);
-                const int t = (int)divide(r, a.by_group);
-                finish_row<N>(a, s.q0 + t, h * a.group + (int)(r - (uint32_t)t * a.group), e0, acc, sum, top);
-            } else {
+        }
+        if constexpr (HW > 1) {
+            // ---- each wavefront's rows: a lane has four elements after another of its row -----
+            // A part lies in the order of these registers, two floats of a lane beside those
+            // of its neighbours.
+            bool finish = whole;
+            if (!whole) {
+                constexpr int MINE = ROWS * DH, ML = HW * MINE;
+                const int at0 = wave * MINE + 2 * lane, at_ml = ML + wave * 2 * ROWS;
                 float* part = part_at<F>(a, parts, parts.mine);
 #pragma unroll
-                for (int e = 0; e < N; e += 2) put2(part + mine * DH + e0 + e, acc[e], acc[e + 1]);
-                if (e0 == 0) put2(part + ROWS * DH + 2 * mine, top, sum);
-            }
-        }
-        if (!whole && last_to_arrive(a, parts, &flag)) {
-            // all parts in their order, four of them on their way at a time
-            constexpr int U = 4;
-            for (int mine = row; mine < rows; mine += 16) {
-                float top = minus_inf(), sum = 0.f, acc[N] = {};
-                for (int i0 = 0; i0 < parts.count; i0 += U) {
-                    float2 ml_i[U], v[U][N / 2];
+                for (int i = 0; i < RT; ++i) {
 #pragma unroll
-                    for (int i = 0; i < U; ++i) {
-                        const float* q = part_at<F>(a, parts, min(i0 + i, parts.count - 1));
-                        ml_i[i] = get2(q + ROWS * DH + 2 * mine);
+                    for (int d = 0; d < DT; ++d)
 #pragma unroll
-                        for (int e = 0; e < N; e += 2) v[i][e / 2] = get2(q + mine * DH + e0 + e);
+                        for (int v = 0; v < 4; v += 2) put2(part + at0 + ((i * DT + d) * 2 + v / 2) * 128, o[i][d][v], o[i][d][v + 1]);
+                    if (grp == 0) put2(part + at_ml + 2 * (16 * i + col), m[i], l[i]);
+                }
+                finish = last_to_arrive(a, parts, &flag);
+                if (finish) {
+                    // all parts in their order, some of them on their way at a time
+#pragma unroll 1
+                    for (int i = 0; i < RT; ++i) {
+                        constexpr int U = 4;
+                        float top = minus_inf(), sum = 0.f;
+                        f32x4 acc[DT];
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        for (int n0 = 0; n0 < parts.count; n0 += U) {
+                            float2 ml_n[U], v[U][DT][2];
+#pragma unroll
+                            for (int n = 0; n < U; ++n) {
+                                const float* q = part_at<F>(a, parts, min(n0 + n, parts.count - 1));
+                                ml_n[n] = get2(q + at_ml + 2 * (16 * i + col));
+#pragma unroll
+                                for (int d = 0; d < DT; ++d) {
+                                    v[n][d][0] = get2(q + at0 + (i * DT + d) * 256);
+                                    v[n][d][1] = get2(q + at0 + (i * DT + d) * 256 + 128);
+                                }
+                            }
+#pragma unroll
+                            for (int n = 0; n < U; ++n) {
+                                if (n0 + n >= parts.count) break;
+                                const float m1 = fmaxf(top, ml_n[n].x), z = m1 == minus_inf() ? 0.f : m1;
+                                const float g0 = exp2_(top - z), g = exp2_(ml_n[n].x - z);
+                                top = m1;
+                                sum = fmaf(ml_n[n].y, g, sum * g0);
+#pragma unroll
+                                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) acc[d][e] = fmaf(e & 1 ? v[n][d][e / 2].y : v[n][d][e / 2].x, g, acc[d][e] * g0);
+                            }
+                        }
+                        const uint32_t r = (uint32_t)(rt * ROWS + 16 * i + col);
+                        const int tok = (int)divide(r, a.by_group);
+                        if (16 * i + col < rows) {
+#pragma unroll
+                            for (int d = 0; d < DT; ++d) {
+                                const float e[4] = {acc[d][0], acc[d][1], acc[d][2], acc[d][3]};
+                                finish_row<4>(a, s.q0 + tok, h * a.group + (int)(r - (uint32_t)tok * a.group), 16 * d + 4 * grp, e, sum, top);
+                            }
+                        }
                     }
+                    joined(a, parts);
+                }
+            } else {
 #pragma unroll
-                    for (int i = 0; i < U; ++i) {
-                        if (i0 + i >= parts.count) break;
-                        const float m1 = fmaxf(top, ml_i[i].x), z = m1 == minus_inf() ? 0.f : m1;
-                        const float f = exp2_(top - z), g = exp2_(ml_i[i].x - z);
-                        top = m1;
-                        sum = fmaf(ml_i[i].y, g, sum * f);
+                for (int i = 0; i < RT; ++i) {
+                    const uint32_t r = (uint32_t)(rt * ROWS + 16 * i + col);
+                    const int tok = (int)divide(r, a.by_group);
+                    if (16 * i + col < rows) {
 #pragma unroll
-                        for (int e = 0; e < N; e += 2) {
-                            acc[e] = fmaf(v[i][e / 2].x, g, acc[e] * f);
-                            acc[e + 1] = fmaf(v[i][e / 2].y, g, acc[e + 1] * f);
+                        for (int d = 0; d < DT; ++d) {
+                            const float e[4] = {o[i][d][0], o[i][d][1], o[i][d][2], o[i][d][3]};
+                            finish_row<4>(a, s.q0 + tok, h * a.group + (int)(r - (uint32_t)tok * a.group), 16 * d + 4 * grp, e, l[i], m[i]);
                         }
                     }
                 }
-                const uint32_t r = (uint32_t)(rt * ROWS + mine);
-                const int t = (int)divide(r, a.by_group);
-                finish_row<N>(a, s.q0 + t, h * a.group + (int)(r - (uint32_t)t * a.group), e0, acc, sum, top);
             }
-            joined(a, parts);
+        } else {
+            // ---- the four wavefronts' parts, a tile of rows after another --------------------
+            constexpr int N = DH / 16;                // elements of a thread
+            float* red = reinterpret_cast<float*>(smem);
+            auto row_of = [&](int mine, int& t, int& head) {     // whether there is one, its token and head
+                const uint32_t r = (uint32_t)(rt * ROWS + mine);
+                t = (int)divide(r, a.by_group);
+                head = h * a.group + (int)(r - (uint32_t)t * a.group);
+                return mine < rows;
+            };
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const int row = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * N;
+                __syncthreads();
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+                    *reinterpret_cast<f32x4*>(red + (wave * 16 + col) * PAD + 16 * d + 4 * grp) = o[i][d];
+                if (grp == 0) {
+                    ml[wave][0][col] = m[i];
+                    ml[wave][1][col] = l[i];
+                }
+                __syncthreads();
+                float top = minus_inf();
+#pragma unroll
+                for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][0][row]);
+                const float zero = top == minus_inf() ? 0.f : top;
+                float sum = 0.f, acc[N] = {};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float g = exp2_(ml[w][0][row] - zero);
+                    sum = fmaf(ml[w][1][row], g, sum);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) acc[e] = fmaf(red[(w * 16 + row) * PAD + e0 + e], g, acc[e]);
+                }
+                int t, head;
+                if (!row_of(16 * i + row, t, head)) continue;
+                if (whole) {
+                    finish_row<N>(a, s.q0 + t, head, e0, acc, sum, top);
+                } else {
+                    float* part = part_at<F>(a, parts, parts.mine);
+#pragma unroll
+                    for (int e = 0; e < N; e += 2) put2(part + (16 * i + row) * DH + e0 + e, acc[e], acc[e + 1]);
+                    if (e0 == 0) put2(part + ROWS * DH + 2 * (16 * i + row), top, sum);
+                }
+            }
+            if (!whole && last_to_arrive(a, parts, &flag)) {
+                // all parts in their order, eight of them on their way at a time; a thread has
+                // four elements of a row
+                constexpr int U = 8;
+                for (int n = threadIdx.x; n < ROWS * (DH / 4); n += kFewThreads) {
+                    const int mine = n / (DH / 4), e0 = n % (DH / 4) * 4;
+                    int t, head;
+                    if (!row_of(mine, t, head)) continue;
+                    float top = minus_inf(), sum = 0.f, acc[4] = {};
+                    for (int i0 = 0; i0 < parts.count; i0 += U) {
+                        float2 ml_i[U], v[U][2];
+#pragma unroll
+                        for (int i = 0; i < U; ++i) {
+                            const float* q = part_at<F>(a, parts, min(i0 + i, parts.count - 1));
+                            ml_i[i] = get2(q + ROWS * DH + 2 * mine);
+                            v[i][0] = get2(q + mine * DH + e0);
+                            v[i][1] = get2(q + mine * DH + e0 + 2);
+                        }
+#pragma unroll
+                        for (int i = 0; i < U; ++i) {
+                            if (i0 + i >= parts.count) break;
+                            const float m1 = fmaxf(top, ml_i[i].x), z = m1 == minus_inf() ? 0.f : m1;
+                            const float f0 = exp2_(top - z), g = exp2_(ml_i[i].x - z);
+                            top = m1;
+                            sum = fmaf(ml_i[i].y, g, sum * f0);
+                            acc[0] = fmaf(v[i][0].x, g, acc[0] * f0);
+                            acc[1] = fmaf(v[i][0].y, g, acc[1] * f0);
+                            acc[2] = fmaf(v[i][1].x, g, acc[2] * f0);
+                            acc[3] = fmaf(v[i][1].y, g, acc[3] * f0);
+                        }
+                    }
+                    finish_row<4>(a, s.q0 + t, head, e0, acc, sum, top);
+                }
+                joined(a, parts);
+            }
         }
         __syncthreads();
-        u += step1 - step0;
+        u += part1 - part0;
     }
 }
 
@@ -453,13 +620,6 @@ __global__ __launch_bounds__(kFewThreads, (kFewPerCu8<DH, RT>)) void attend8_few
 // Values' scales that are powers of two go into the widening, which is exact, else
 // they multiply the weights.  Keys' scales multiply scores, in the multiply-add that
 // takes the maximum off.
-// Whether a scale is a power of two (and a normal number) by which widening is exact.
-__device__ __forceinline__ bool is_power(float s)
-{
-    const uint32_t w = __float_as_uint(s);
-    return (w & 0x807fffffu) == 0 && w - (10u << 23) < (238u << 23);       // 2^-117 .. 2^120
-}
-
 // UNI: pages and blocks of whole 16 tokens, so that a scale is that of 16 keys.
 template <int DH, int NW, int STEP, bool UNI, bool FULL>
 __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kernel(Attend8Args a)
@@ -522,14 +682,7 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
             u32x4 v{};
             if (live && (FULL || k * 16 + half * 8 < a.dim))
                 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q.p) + (s.q0 + tok) * a.q.token + (int64_t)head * a.q.head + k * 16 + half * 8);
-            // scale < 0: that of -q; scale 0: scores of q = 0, NaN where it is not finite
-            if (a.keep == 0) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[i] = ((v[i] & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u);
-            }
-            v ^= a.flip;
-            qf[k] = __builtin_bit_cast(bf16x8, v);
+            qf[k] = signed_query(a, v);
         }
         f32x16 o[DT];
 #pragma unroll
@@ -584,8 +737,8 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
                 const float by = value && folded ? f : 1.f;
                 const int turn = value ? v_swizzle<DH>(row) : k_swizzle<DH>(row);
                 unsigned char* to = smem + stage * 2 * BYTES + (value ? BYTES : 0) + row * (DH * 2);
-                *reinterpret_cast<bf16x8*>(to + (piece ^ turn) * 16) = widen8(raw[i].x, raw[i].y, by);
-                *reinterpret_cast<bf16x8*>(to + ((piece + 1) ^ turn) * 16) = widen8(raw[i].z, raw[i].w, by);
+                *reinterpret_cast<bf16x8*>(to + (piece ^ turn) * 16) = widen8(raw[i].x, raw[i].y, by, by);
+                *reinterpret_cast<bf16x8*>(to + ((piece + 1) ^ turn) * 16) = widen8(raw[i].z, raw[i].w, by, by);
             }
         };
         float ks = 0.f, vs = 0.f;
@@ -655,9 +808,7 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
                         sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], sc[x], 0, 0, 0);
                     }
                 }
-                // Factors of the scores.  Those of keys that no row sees may be anything; 0
-                // would make NaN of -inf, which the smallest normal number does not.
-                const float by = fmaxf(ks * a.scale, 0x1p-126f);
+                const float by = factor(ks * a.scale);
                 float f[4];
                 if constexpr (UNI) {
 #pragma unroll
@@ -871,17 +1022,30 @@ bool in_halves(const Attend8Args& a)
            a.cache8.token * (int64_t)a.cache8.page_size < INT32_MAX;
 }
 
+template <int DH, int HW, int RT>
+hipError_t few(const Attend8Args& args, hipStream_t s)
+{
+    Attend8Args a = args;
+    a.kv_heads /= HW;
+    const bool pg16 = in_halves(a);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)a.cus), dim3(kFewThreads), 0, s, a);
+        return hipGetLastError();
+    };
+    if (a.dim == DH) return pg16 ? launch(attend8_few_kernel<DH, HW, RT, true, true>) : launch(attend8_few_kernel<DH, HW, RT, false, true>);
+    return pg16 ? launch(attend8_few_kernel<DH, HW, RT, true, false>) : launch(attend8_few_kernel<DH, HW, RT, false, false>);
+}
+
+// Four heads to a workgroup where their rows are shorter than memory's lines and lie
+// side by side, and there are enough of them that a workgroup need not begin and end
+// many (one request of 32 heads of 64 over 1216 tokens: 12 us and 21).
 template <int DH, int RT>
 hipError_t few(const Attend8Args& a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(kFewPerCu8<DH, RT> * a.cus));
-    const bool pg16 = in_halves(a);
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kFewThreads), 0, s, a);
-        return hipGetLastError();
-    };
-    if (a.dim == DH) return pg16 ? launch(attend8_few_kernel<DH, RT, true, true>) : launch(attend8_few_kernel<DH, RT, false, true>);
-    return pg16 ? launch(attend8_few_kernel<DH, RT, true, false>) : launch(attend8_few_kernel<DH, RT, false, false>);
+    if constexpr (DH == 64) {
+        if (a.kv_heads % 4 == 0 && a.cache8.head < 128 && a.step.seqs * (a.kv_heads / 4) >= a.cus / 8) return few<DH, 4, RT>(a, s);
+    }
+    return few<DH, 1, RT>(a, s);
 }
 
 // Wavefronts of a workgroup of the kernel for many rows.
@@ -917,16 +1081,19 @@ hipError_t attend8(const Attend8Args& args, hipStream_t s)
 {
     Attend8Args a = args;
     const int64_t rows = a.tokens * a.group;
-    if (rows <= 64 * (int64_t)a.step.seqs) {
-        a.scale = a.raw_scale * kLog2e;
-        if (rows <= 16 * (int64_t)a.step.seqs) return few<DH, 1>(a, s);
-        if (rows <= 32 * (int64_t)a.step.seqs || DH == 256) return few<DH, 2>(a, s);
-        if constexpr (DH < 256) return few<DH, 4>(a, s);
-    }
     a.scale = fabsf(a.raw_scale) * kLog2e;
     a.flip = a.raw_scale < 0.f ? 0x80008000u : 0u;
     a.keep = a.scale > 0.f ? ~0u : 0u;
     if (!a.keep) a.scale = 1.f;
+    // By the rows of a sequence and key head, on average (16 requests with 5 to 9 tokens,
+    // groups of 8, heads of 128: 79 us with four tiles of rows, 166 as many; 64 with 2 to 4,
+    // groups of 7: 140 with two, 193 with four).
+    const int64_t seqs = a.step.seqs;
+    if (rows <= 16 * seqs) return few<DH, 1>(a, s);
+    if (rows <= 32 * seqs) return few<DH, 2>(a, s);
+    if constexpr (DH < 256) {
+        if (rows <= 64 * seqs) return few<DH, 4>(a, s);
+    }
     return many<DH>(a, s);
 }
 

@@ -114,11 +114,11 @@ __device__ __forceinline__ int tiles_of(const AttendArgs& a, const Sequence& s)
 }
 
 template <int ROWS, int STEP>
-__device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b)
+__device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b, int extra)
 {
     if (b >= a.step.seqs) return 0;
     const Sequence s = sequence_at(a, b);
-    return (int64_t)tiles_of<ROWS>(a, s) * steps_of<STEP>(s) * a.kv_heads;
+    return (int64_t)tiles_of<ROWS>(a, s) * (steps_of<STEP>(s) + extra) * a.kv_heads;
 }
 
 // All steps, and a workgroup's share of them: at least 1 / kMostParts of the
@@ -128,6 +128,7 @@ constexpr int kMostParts = 64;
 
 struct Shares {
     int64_t total, share;
+    int extra;         // steps that an item counts for besides its own (first_place)
 };
 
 template <int ROWS, int STEP>
@@ -153,6 +154,7 @@ __device__ __forceinline__ Shares shares_of(const AttendArgs& a, int lane)
     r.total = uniform(sum);
     r.share = max((r.total + gridDim.x - 1) / gridDim.x,
                   (int64_t)((__builtin_amdgcn_readfirstlane(most) + kMostParts - 1) / kMostParts));
+    r.extra = 0;
     return r;
 }
 
@@ -166,11 +168,11 @@ constexpr int kSearched = 128;
 // on, before which lie `before` (<= u) steps: a workgroup walks the sequences of
 // its share once.
 template <int ROWS, int STEP>
-__device__ __forceinline__ Place place_of(const AttendArgs& a, int64_t u, int lane, int from = 0, int64_t before = 0)
+__device__ __forceinline__ Place place_of(const AttendArgs& a, int64_t u, int lane, int from = 0, int64_t before = 0, int extra = 0)
 {
     Place p{};
     for (int b0 = from; b0 < a.step.seqs; b0 += 64) {
-        const int64_t c = cost_of<ROWS, STEP>(a, b0 + lane);
+        const int64_t c = cost_of<ROWS, STEP>(a, b0 + lane, extra);
         int64_t sum = c;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -188,9 +190,66 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int64_t u, int la
     }
     p.b = __builtin_amdgcn_readfirstlane(p.b);
     p.s = sequence_at(a, p.b);
-    p.steps = steps_of<STEP>(p.s);
+    p.steps = steps_of<STEP>(p.s) + extra;
     p.tiles = tiles_of<ROWS>(a, p.s);
     return p;
+}
+
+// shares_of, and where the workgroup's share begins, with each sequence looked at once
+// where a wavefront can (up to 64 of them).  To begin an item and to end it takes a
+// workgroup about as long as kItemSteps steps; where shares are long each item counts
+// for so many more, at its beginning.  A share has at least LEAST steps.
+constexpr int kItemSteps = 3, kLongShare = 8;
+
+template <int ROWS, int STEP, int LEAST>
+__device__ __forceinline__ Shares first_place(const AttendArgs& a, int lane, Place& p)
+{
+    if (a.step.seqs > 64) {
+        Shares all = shares_of<ROWS, STEP>(a, lane);
+        all.share = max(all.share, (int64_t)LEAST);
+        const int64_t u = (int64_t)blockIdx.x * all.share;
+        if (u < all.total) p = place_of<ROWS, STEP>(a, u, lane);
+        return all;
+    }
+    Sequence s{};
+    int64_t cost = 0, items = 0;
+    int steps = 0;
+    if (lane < a.step.seqs) {
+        s = sequence_at(a, lane);
+        steps = steps_of<STEP>(s);
+        items = (int64_t)tiles_of<ROWS>(a, s) * a.kv_heads;
+        cost = items * steps;
+    }
+    int64_t sum = cost, all_items = items;
+    int most = s.n > 0 ? steps : 0;               // those without new tokens have no items
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int64_t o = __shfl_up(sum, m), i = __shfl_up(all_items, m);
+        if (lane >= m) {
+            sum += o;
+            all_items += i;
+        }
+        most = max(most, __shfl_xor(most, m));
+    }
+    Shares r;
+    r.total = uniform(__shfl(sum, 63));
+    r.extra = r.total >= (int64_t)kLongShare * gridDim.x ? kItemSteps : 0;
+    sum += all_items * r.extra;
+    cost += items * r.extra;
+    r.total = uniform(__shfl(sum, 63));
+    r.share = max(max((r.total + gridDim.x - 1) / gridDim.x, (int64_t)LEAST),
+                  (int64_t)((__builtin_amdgcn_readfirstlane(most) + r.extra + kMostParts - 1) / kMostParts));
+    const uint64_t past = __ballot((int64_t)blockIdx.x * r.share < sum);
+    p.b = past ? __builtin_ctzll(past) : 0;
+    auto from = [&](int x) { return __builtin_amdgcn_readlane(x, p.b); };
+    p.first = uniform(__shfl(sum - cost, p.b));
+    p.steps = from(steps) + r.extra;
+    p.s.q0 = uniform(__shfl(s.q0, p.b));
+    p.s.n = from(s.n);
+    p.s.len = from(s.len);
+    p.s.begin = from(s.begin);
+    p.s.end = from(s.end);
+    return r;
 }
 
 // N elements from e0 of one finished row: sums over their l, and lse from the
