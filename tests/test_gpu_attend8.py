@@ -193,8 +193,30 @@ def test_rows_of_no_sequence_stay():
         assert ((o - want[2:5]).abs() <= 2.0 ** -8 * want[2:5].abs() + (2.0 ** -8 + 1.5e-3) * mass[2:5]).all()
 
 
+@pytest.mark.parametrize("dim", [64, 48, 16])
+@pytest.mark.parametrize("most", [1, 4, 9])
+def test_heads_side_by_side(dim, most):
+    """Enough sequences that a workgroup takes four heads at a time, of one to some tiles
+    of rows; layouts in which they do and do not lie side by side."""
+    for kv_heads, page_size, block, layout, window, powers in ((4, 16, 16, "rows", 0, True), (8, 64, 32, "rows", 50, False), (4, 24, 8, "rows", 0, False),
+                                                               (4, 32, 16, "heads", 0, True), (8, 16, 16, "joined", 7, True)):
+        say("side by side", dim, most, kv_heads, page_size, layout)
+        g = gen(dim + most + kv_heads)
+        new = [1 + i % most for i in range(40)]
+        kv = [n + int(x) for n, x in zip(new, torch.randint(0, 300, (40,), generator=g))]
+        kv[3], kv[17] = 5000, new[17]
+        new[9] = 0
+        step, pages = step_of(new, kv, page_size, g)
+        a = tr.Attention(4 * kv_heads, kv_heads, dim, BF)
+        compare(a, queries(g, sum(new), 4 * kv_heads, dim), cache8(pages, page_size, kv_heads, dim, g, block, layout, powers), step, window=window,
+                what=(dim, most, kv_heads, layout))
+        a.close()
+
+
 # new tokens, lengths, heads, key heads, causal: each kernel and its ways of dealing the work
-KERNELS = {"single": ([1, 1], [700, 90], 4, 2, True), "drafts": ([3, 8], [700, 90], 4, 2, True), "shares": ([70, 130], [701, 300], 4, 2, False),
+KERNELS = {"four": ([1] * 33 + [2], [40 + 9 * i for i in range(34)], 12, 4, True), "four_of_two": ([6] * 34, [70 + 9 * i for i in range(34)], 16, 4, True),
+           "four_of_four": ([13] * 34, [70 + 19 * i for i in range(34)], 16, 4, False),
+           "single": ([1, 1], [700, 90], 4, 2, True), "drafts": ([3, 8], [700, 90], 4, 2, True), "shares": ([70, 130], [701, 300], 4, 2, False),
            "in_turn": ([1200], [1200], 80, 80, True), "items": ([2048], [2050], 64, 64, True)}
 
 

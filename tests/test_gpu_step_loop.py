@@ -1,0 +1,129 @@
+"""A server's steps as they follow one another: tables, new keys and values into the 8-bit
+cache, attention, verification of drafts, whose rejected tokens leave the tables again."""
+import pytest
+import torch
+
+import attn_ref as ref
+import paper_2607_13500_amd as tr
+import test_gpu_pages as pages_
+import test_gpu_verify as verify_
+from test_gpu_attend8 import cache8, stands_for
+from test_gpu_rotate import BF, DEV, gen, say
+
+pytestmark = pytest.mark.gpu
+
+I32 = torch.int32
+
+
+def test_steps_of_drafts():
+    """Requests that begin with prompts of different lengths, then steps of drafts; one
+    ends on the way and its pages are taken by others.  Each call against its own
+    definition on what the others left."""
+    g = gen(3)
+    seqs, size, width, pages, vocab, heads, kv_heads, dim, most = 5, 16, 12, 34, 90, 8, 2, 64, 4
+    a = tr.Attention(heads, kv_heads, dim, BF, norm=True)
+    wq, wk = ((1 + 0.2 * torch.randn(dim, generator=g)).to(BF).to(DEV) for _ in range(2))
+    cache = cache8(pages, size, kv_heads, dim, g)
+    kv = torch.zeros(seqs, dtype=I32, device=DEV)
+    table = torch.full((seqs, width), -1, dtype=I32, device=DEV)
+    pool = tr.PagePool(torch.randperm(pages, generator=g).to(I32).to(DEV), torch.tensor([0, pages], dtype=I32, device=DEV))
+    change = torch.tensor([40, 7, 0, 90, 16], dtype=I32, device=DEV)
+    lengths, accepted_in_all = [0] * seqs, 0
+    for step in range(14):
+        say("step", step)
+        room = int(change.clamp(min=0).sum()) + 3
+        want = pages_.plain(change.tolist(), kv.tolist(), table.tolist(), pool.ring.tolist(), pool.state.tolist(), size, room)
+        u = tr.update_pages(change, kv, table, pool, size, room, in_place=True)
+        assert u.short.tolist() == [0] and u.slots.tolist() == want["slots"] and u.pos.tolist() == want["pos"] and table.tolist() == want["table"]
+        lengths = [max(0, n + c) for n, c in zip(lengths, change.tolist())]
+        assert kv.tolist() == lengths
+        x = torch.randn(room, heads + 2 * kv_heads, dim, generator=g).to(BF).to(DEV)
+        q, k, v = x.split([heads, kv_heads, kv_heads], 1)
+        out = torch.full((room, heads, dim), 7.0, dtype=BF, device=DEV)
+        rq = a.append(q, k, v, u.pos, cache, u.step, wq=wq, wk=wk)
+        a.attend(rq, cache, u.step, out=out)
+        rows = int(u.step.q_start[-1])
+        on_cpu = tr.Step(*(t.cpu() for t in u.step))
+        o, _, mass, _ = ref.attend(rq.cpu()[:rows], *stands_for(cache), on_cpu, dim ** -0.5, True, 0)
+        assert ((out.cpu().double()[:rows] - o).abs() <= 2.0 ** -8 * o.abs() + (2.0 ** -8 + 1.5e-3) * mass).all()
+        assert (out[rows:] == 7.0).all()
+        # the newest keys are those of the last rows: within a rounding of what rotation gives
+        rk = a.rotate(None, k, u.pos, wk=wk)[1].float()
+        flat = stands_for(cache)[0].flatten(0, 1).to(DEV)
+        newest = flat[u.slots[:rows]].float()
+        scale = cache.k_scale.repeat_interleave(size // cache.k_scale.shape[1], 1).flatten(0, 1)[u.slots[:rows]]
+        assert ((newest - rk[:rows]).abs() <= (2.0 ** -4 + 2.0 ** -8) * rk[:rows].abs() + 2.0 ** -10 * scale[..., None] + 1e-5).all()
+
+        counts = (u.step.q_start[1:] - u.step.q_start[:-1]).tolist()
+        target, ids, accept, draw, draft = verify_.inputs(g, counts, vocab, torch.float32, True)
+        verified = verify_.check(target, ids, counts, accept, draw, max(counts), draft)
+        accepted_in_all += int(verified.accepted.sum())
+        if step == 0:                              # prompts stay; the first drafts come
+            change = torch.tensor([most, 1, most - 1, most, 2], dtype=I32, device=DEV)
+            continue
+        back = tr.update_pages(verified.change, kv, table, pool, size, 0, in_place=True)
+        assert back.short.tolist() == [0] and back.step.q_start.tolist() == [0] * (seqs + 1)
+        lengths = [n + c for n, c in zip(lengths, verified.change.tolist())]
+        assert kv.tolist() == lengths
+        change = torch.randint(1, most + 1, (seqs,), generator=g).to(I32).to(DEV)
+        if step == 6:
+            change[3] = -1000                      # a request ends
+        held = [p for r, n in zip(table.tolist(), lengths) for p in r[:pages_.pages_for(n, size)]]
+        first, free = pool.state.tolist()
+        assert sorted(held + [pool.ring.tolist()[(first + i) % pages] for i in range(free)]) == list(range(pages))
+    assert accepted_in_all > 20
+
+
+def test_a_step_replays_from_a_graph():
+    """Tables, append, attention and verification of a step recorded together: each
+    replay leaves the bits of the eager calls."""
+    g = gen(8)
+    seqs, size, pages, vocab, heads, kv_heads, dim, most = 6, 16, 60, 50001, 4, 4, 128, 3
+    a = tr.Attention(heads, kv_heads, dim, BF)
+
+    def state():
+        h = gen(9)
+        return {"kv": torch.zeros(seqs, dtype=I32, device=DEV), "table": torch.zeros(seqs, 10, dtype=I32, device=DEV),
+                "pool": tr.PagePool(torch.arange(pages, dtype=I32, device=DEV), torch.tensor([0, pages], dtype=I32, device=DEV)),
+                "cache": cache8(pages, size, kv_heads, dim, h)}
+
+    rows = seqs * most
+    x = torch.zeros(rows, heads + 2 * kv_heads, dim, dtype=BF, device=DEV)
+    change = torch.zeros(seqs, dtype=I32, device=DEV)
+    target, draft = (torch.zeros(rows, vocab, device=DEV) for _ in range(2))
+    ids, accept, draw = torch.zeros(rows, dtype=I32, device=DEV), torch.zeros(rows, device=DEV), torch.zeros(seqs, device=DEV)
+
+    def call(s):
+        u = tr.update_pages(change, s["kv"], s["table"], s["pool"], size, rows, in_place=True)
+        q = a.append(x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:], u.pos, s["cache"], u.step)
+        out, lse = a.attend(q, s["cache"], u.step, out=torch.zeros(rows, heads, dim, dtype=BF, device=DEV))
+        v = tr.verify_drafts(target, ids, u.step.q_start, accept, draw, most, draft=draft)
+        back = tr.update_pages(v.change, s["kv"], s["table"], s["pool"], size, 0, in_place=True)
+        return [u.slots, u.pos, u.short, u.step.q_start, out, *v, back.short]
+
+    eager, recorded = state(), state()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call(state())
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call(recorded)
+    for i in range(8):
+        change.copy_(torch.randint(1, most + 1, (seqs,), generator=g).to(I32) if i else torch.full((seqs,), most, dtype=I32))
+        x.copy_(torch.randn(x.shape, generator=g).to(BF))
+        target.copy_(torch.softmax(3 * torch.randn(target.shape, generator=g), 1))
+        draft.copy_(torch.softmax(3 * torch.randn(draft.shape, generator=g), 1))
+        ids.copy_(torch.randint(0, vocab, (rows,), generator=g).to(I32))
+        accept.copy_(torch.rand(rows, generator=g))
+        draw.copy_(torch.rand(seqs, generator=g))
+        want = call(eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, (x1, x2) in enumerate(zip(got, want)):
+            assert torch.equal(x1, x2), (i, n)
+        for name in ("kv", "table"):
+            assert torch.equal(eager[name], recorded[name])
+        for x1, x2 in zip(eager["cache"] + eager["pool"], recorded["cache"] + recorded["pool"]):
+            assert torch.equal(x1.view(torch.uint8), x2.view(torch.uint8)), i

@@ -148,14 +148,17 @@ def test_width_cuts_drafts_off():
         assert v.accepted.tolist() == [min(n, width) - 1 for n in rows]
 
 
-def test_borders():
+SMALL_AND_LARGE = pytest.mark.parametrize("vocab", [300, 41003])      # one launch, and two
+
+
+@SMALL_AND_LARGE
+def test_borders(vocab):
     """Numbers at the ends of their range and out of it, weights of 0 at both ends, all
     mass on one word, equal distributions, none at all."""
-    say("borders")
-    vocab = 300
+    say("borders", vocab)
     one = torch.zeros(1, vocab)
     cases = []
-    for first, last in ((0, 299), (7, 7), (299, 299), (0, 0), (100, 200)):
+    for first, last in ((0, vocab - 1), (7, 7), (vocab - 1, vocab - 1), (0, 0), (100, 200), (vocab - 150, vocab - 1)):
         p = one.clone()
         p[0, first:last + 1] = 0.25
         for u, want in ((0.0, first), (1.0 - 2.0 ** -24, last), (1.0, last), (5.0, last), (-1.0, first), (math.nan, first)):
@@ -182,19 +185,20 @@ def test_borders():
         assert v.tokens.tolist() == [[want]]
 
 
-def test_improper_probabilities():
+@SMALL_AND_LARGE
+def test_improper_probabilities(vocab):
     """NaN, negative and infinite ones count as 0, drafts that are no words are rejected."""
-    say("improper")
+    say("improper", vocab)
     g = gen(9)
     rows = [3, 4, 2]
     for dtype in (F32, BF):
         for with_draft in (True, False):
-            t, i, a, d, q = inputs(g, rows, 100, dtype, with_draft)
+            t, i, a, d, q = inputs(g, rows, vocab, dtype, with_draft)
             for n, bad in enumerate((math.nan, -0.5, math.inf, -math.inf)):
                 t[:, 5 + n] = bad
                 if with_draft:
                     q[:, 6 + n] = bad
-            i[1], i[4], i[8] = -1, 100, 5
+            i[1], i[4], i[8] = -1, vocab, 5
             check(t, i, rows, a, d, 4, q)
             t.fill_(math.nan)
             v = check(t, i, rows, a, d, 4, q)
@@ -207,7 +211,7 @@ def test_rows_anywhere():
     g = gen(10)
     rows = [3, 2, 5]
     for dtype in (F32, BF):
-        for vocab in (64, 333):
+        for vocab in (64, 333, 41005):
             t, i, a, d, q = inputs(g, rows, vocab, dtype, True)
             want = check(t, i, rows, a, d, 5, q)
             wide = torch.full((13, vocab + 5), math.nan, dtype=dtype, device=DEV)
@@ -231,10 +235,11 @@ def test_row_starts_out_of_range():
     assert (v.tokens == -1).all() and not v.accepted.any() and not v.change.any()
 
 
-def test_replays_from_a_graph():
+@SMALL_AND_LARGE
+def test_replays_from_a_graph(vocab):
     g = gen(13)
     rows = [3, 1, 4]
-    t, i, a, d, q = (x.to(DEV) for x in inputs(g, rows, 4000, F32, True))
+    t, i, a, d, q = (x.to(DEV) for x in inputs(g, rows, vocab, F32, True))
     start = torch.tensor([0, 3, 4, 8], dtype=I32, device=DEV)
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
@@ -244,7 +249,7 @@ def test_replays_from_a_graph():
     with torch.cuda.graph(graph):
         v = tr.verify_drafts(t, i, start, a, d, 4, draft=q)
     for n in range(5):
-        new = inputs(g, rows, 4000, F32, True)
+        new = inputs(g, rows, vocab, F32, True)
         for old, x in zip((t, i, a, d, q), new):
             old.copy_(x)
         want = check(*(new[0], new[1], rows, new[2], new[3], 4, new[4]))
