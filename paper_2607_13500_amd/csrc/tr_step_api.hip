@@ -47,6 +47,8 @@ tr_status tr_update_pages(int32_t seqs, const int32_t* change, const int32_t* kv
         return fail(TR_EUNSUPPORTED, "int32 arrays must be 4-byte and slots 8-byte aligned");
     if (crosses(kv_len, kv_out, 4 * (int64_t)seqs) || crosses(pool->state, pool->state_out, 8))
         return fail(TR_EINVAL, "kv_out and state_out must be kv_len and state themselves or apart from them");
+    if (crosses(change, kv_out, 4 * (int64_t)seqs) || (seqs && change == kv_out && kv_out != kv_len))
+        return fail(TR_EINVAL, "kv_out must not share memory with change");
     tr::PagesArgs a{};
     a.seqs = seqs;
     a.change = change;

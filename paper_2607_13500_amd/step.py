@@ -100,8 +100,9 @@ def update_pages(change: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor
         raise ValueError("pool.ring must be an int32 [pages] tensor on cuda:%d" % index)
     pages = ring.shape[0]
     at_ring, at_state = _vector("pool.ring", ring, index, _I32, pages), _vector("pool.state", state, index, _I32, 2)
-    if rows < 0:
-        raise ValueError("rows must be >= 0 (got %d)" % rows)
+    page_size = int(page_size)
+    if rows < 0 or not 0 < page_size < 1 << 31:
+        raise ValueError("rows must be >= 0 (got %d) and page_size in [1, 2^31 - 1] (got %d)" % (rows, page_size))
     sizes = [seqs + 1, rows, 1] if in_place else [seqs + 1, rows, 1, seqs, 2]
     parts = _empty((sum(sizes),), _I32, kv_len.device, stream).unsafe_split_with_sizes(sizes)
     q_start, pos, short = parts[:3]
@@ -109,7 +110,7 @@ def update_pages(change: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor
     slots = _empty((rows,), _I64, kv_len.device, stream)
     p = Pool(pages, at_ring, at_state, state_out.data_ptr())
     _run(_lib.load().tr_update_pages, "tr_update_pages", index, stream, seqs, at_change, at_kv, kv_out.data_ptr(), at_table, width, row,
-         int(page_size), ctypes.byref(p), q_start.data_ptr(), rows, slots.data_ptr(), pos.data_ptr(), short.data_ptr())
+         page_size, ctypes.byref(p), q_start.data_ptr(), rows, slots.data_ptr(), pos.data_ptr(), short.data_ptr())
     return PageUpdate(Step(q_start, kv_out, table), slots, pos, PagePool(ring, state_out), short)
 
 
@@ -136,8 +137,8 @@ def verify_drafts(target: torch.Tensor, ids: torch.Tensor, q_start: torch.Tensor
     if not isinstance(q_start, torch.Tensor) or q_start.dim() != 1 or q_start.shape[0] < 1:
         raise ValueError("q_start must be an int32 [seqs + 1] tensor on cuda:%d" % index)
     seqs = q_start.shape[0] - 1
-    if width < 1:
-        raise ValueError("width must be >= 1 (got %d)" % width)
+    if not 0 < width < 1 << 31:
+        raise ValueError("width must be in [1, 2^31 - 1] (got %d)" % width)
     p, ld, _ = _matrix("target", target, index, dtype, tokens)
     q, ld_draft = None, 0
     if draft is not None:

@@ -222,6 +222,7 @@ def test_refusals():
            lambda: tr.update_pages(kv, kv.cpu(), table, pool, 16, 4), lambda: tr.update_pages(kv, kv, table[:2], pool, 16, 4),
            lambda: tr.update_pages(kv, kv, table.t()[:3, :3], pool, 16, 4), lambda: tr.update_pages(kv, kv, table[:1].expand(3, 4), pool, 16, 4),
            lambda: tr.update_pages(kv, kv, table, pool, 0, 4), lambda: tr.update_pages(kv, kv, table, pool, 16, -1),
+           lambda: tr.update_pages(kv, kv, table, pool, (1 << 32) + 16, 4), lambda: tr.update_pages(kv, kv, table, pool, 16, 1 << 31),
            lambda: tr.update_pages(kv, kv, table, tr.PagePool(ring[:0], state), 16, 4), lambda: tr.update_pages(kv, kv, table, tr.PagePool(ring.long(), state), 16, 4),
            lambda: tr.update_pages(kv, kv, table, tr.PagePool(ring, state[:1]), 16, 4), lambda: tr.update_pages(kv, kv, table, tr.PagePool(ring[::2], state), 16, 4)]
     for i, f in enumerate(bad):

@@ -286,7 +286,7 @@ def test_refusals():
     i, s, a, d = torch.zeros(4, dtype=I32, device=DEV), torch.tensor([0, 4], dtype=I32, device=DEV), torch.zeros(4, device=DEV), torch.zeros(1, device=DEV)
     bad = [lambda: tr.verify_drafts(t.double(), i, s, a, d, 4), lambda: tr.verify_drafts(t.cpu(), i, s, a, d, 4), lambda: tr.verify_drafts(t, i.long(), s, a, d, 4),
            lambda: tr.verify_drafts(t, i[:3], s, a, d, 4), lambda: tr.verify_drafts(t, i, s.long(), a, d, 4), lambda: tr.verify_drafts(t, i, s[:0], a, d, 4),
-           lambda: tr.verify_drafts(t, i, s, a.double(), d, 4), lambda: tr.verify_drafts(t, i, s, a, a, 4), lambda: tr.verify_drafts(t, i, s, a, d, 0),
+           lambda: tr.verify_drafts(t, i, s, a.double(), d, 4), lambda: tr.verify_drafts(t, i, s, a, a, 4), lambda: tr.verify_drafts(t, i, s, a, d, 0), lambda: tr.verify_drafts(t, i, s, a, d, (1 << 32) + 1),
            lambda: tr.verify_drafts(t, i, s, a, d, 4, draft=t[:, :9]), lambda: tr.verify_drafts(t, i, s, a, d, 4, draft=t.to(BF)),
            lambda: tr.verify_drafts(t.t(), i, s, a, d, 4), lambda: tr.verify_drafts(t[:1].expand(4, 10), i, s, a, d, 4), lambda: tr.verify_drafts(t[:, :0], i, s, a, d, 4)]
     for n, f in enumerate(bad):

@@ -32,7 +32,7 @@ def pages(lib, pool_=None, **bad):
 def test_update_pages_refusals(lib):
     for bad in (dict(seqs=-1), dict(rows=-1), dict(rows=1 << 31), dict(page_size=0), dict(table_width=-1), dict(table_stride=3), dict(table_stride=0),
                 dict(q_start=None), dict(short_of=None), dict(change=None), dict(kv_len=None), dict(kv_out=None), dict(table=None), dict(kv_out=G + 4),
-                dict(kv_out=G - 8), dict(pool=None)):
+                dict(kv_out=G - 8), dict(change=G + 1024, kv_out=G + 1024), dict(change=G + 1024, kv_out=G + 1028), dict(pool=None)):
         assert pages(lib, **bad) == _lib.TR_EINVAL, bad
         assert lib.tr_last_error()
     for bad in (dict(pages=0), dict(ring=None), dict(state=None), dict(state_out=None), dict(state_out=G + 4)):
