@@ -8,7 +8,8 @@
 // new token's page is read from where the page is taken from, not from the table, so
 // that no workgroup waits for another; given pages go behind all free ones, where
 // nothing is taken from.  Bound by latency: two dependent rounds of loads and some
-// barriers.
+// barriers (64 sequences with a token each 3.6 us; 1024 with 1 to 96 tokens, 0.46 MB,
+// 8.8 us; with 64-bit sums by shuffles in workgroups of 1024 threads 13.2 and 17.6).
 #include <algorithm>
 
 #include "tr_step.h"
