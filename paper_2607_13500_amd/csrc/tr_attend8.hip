@@ -633,6 +633,11 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
     constexpr int BYTES = kManyTile * DH * 2;               // of a widened tile
     constexpr int PIECES = DH / 16, NP = kManyTile * PIECES;   // pieces of a row and of a tile, 16 bytes each
     constexpr int NI = 2 * NP / T;                          // of a thread, keys' before values'
+    // Items by themselves widen the next tile's pieces between the first product's
+    // instructions (a prompt of 8192 tokens, 8 heads of 64: 429 us, before it 458; 4 of 256:
+    // 2922 and 3010; 18432 tokens, 8 of 128: 1 %).  Shares widen them before it: between,
+    // chunks of 8 requests with 4 heads of 128 took 550 us and not 530.
+    constexpr bool kBetween = STEP == 0;
     __shared__ __align__(16) unsigned char smem[4 * BYTES]; // stage 0: K, V; stage 1: K, V
     __shared__ int flag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -732,34 +737,27 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
             ks_next = ksp[scale];
             vs_next = vsp[scale];
         };
-        auto store = [&](int stage, bool folded) {
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int n = i * T + (int)threadIdx.x, p = n & (NP - 1), row = p / PIECES, piece = 2 * (p % PIECES);
-                const bool value = n >= NP;
-                const float f = __shfl(vs_next, row);
-                const float by = value && folded ? f : 1.f;
-                const int turn = value ? v_swizzle<DH>(row) : k_swizzle<DH>(row);
-                unsigned char* to = smem + stage * 2 * BYTES + (value ? BYTES : 0) + row * (DH * 2);
-                *reinterpret_cast<bf16x8*>(to + (piece ^ turn) * 16) = widen8(raw[i].x, raw[i].y, by, by);
-                *reinterpret_cast<bf16x8*>(to + ((piece + 1) ^ turn) * 16) = widen8(raw[i].z, raw[i].w, by, by);
-            }
+        auto store = [&](int i, int stage, bool folded) {      // piece i of the tile in registers, into a stage
+            const int n = i * T + (int)threadIdx.x, p = n & (NP - 1), row = p / PIECES, piece = 2 * (p % PIECES);
+            const bool value = n >= NP;
+            const float f = __shfl(vs_next, row);
+            const float by = value && folded ? f : 1.f;
+            const int turn = value ? v_swizzle<DH>(row) : k_swizzle<DH>(row);
+            unsigned char* to = smem + stage * 2 * BYTES + (value ? BYTES : 0) + row * (DH * 2);
+            *reinterpret_cast<bf16x8*>(to + (piece ^ turn) * 16) = widen8(raw[i].x, raw[i].y, by, by);
+            *reinterpret_cast<bf16x8*>(to + ((piece + 1) ^ turn) * 16) = widen8(raw[i].z, raw[i].w, by, by);
         };
-        float ks = 0.f, vs = 0.f;
+        float ks = 0.f, vs = 0.f;                 // of the stage that is read
         bool folded = false;
-        auto take = [&](int stage) {              // the tile in registers becomes that of a stage
-            ks = ks_next;
-            vs = vs_next;
-            folded = __all(is_power(vs)) != 0;
-            store(stage, folded);
-        };
-        float ks_then = 0.f, vs_then = 0.f;       // of the stage that is being filled
-        bool folded_then = false;
         if (j0 < j_end) {
             look(j0);
             fetch();
             if (j0 + kManyTile < j_end) look(j0 + kManyTile);
-            take(0);
+            ks = ks_next;
+            vs = vs_next;
+            folded = __all(is_power(vs)) != 0;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) store(i, 0, folded);
             if (j0 + kManyTile < j_end) {
                 fetch();
                 if (j0 + 2 * kManyTile < j_end) look(j0 + 2 * kManyTile);
@@ -768,20 +766,16 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
         int stage = 0;
         for (; j0 < j_end; j0 += kManyTile, stage ^= 1) {
             __syncthreads();
-            if (j0 + kManyTile < j_end) {
-                const float k0 = ks, v0 = vs;
-                const bool f0 = folded;
-                take(stage ^ 1);
-                ks_then = ks;
-                vs_then = vs;
-                folded_then = folded;
-                ks = k0;
-                vs = v0;
-                folded = f0;
-                if (j0 + 2 * kManyTile < j_end) {
-                    fetch();
-                    if (j0 + 3 * kManyTile < j_end) look(j0 + 3 * kManyTile);
-                }
+            const float ks_then = ks_next, vs_then = vs_next;       // of the stage that is filled
+            const bool folded_then = __all(is_power(vs_then)) != 0;
+            auto ahead = [&] {                    // past the last tile: its keys again
+                fetch();
+                look(j0 + 3 * kManyTile);
+            };
+            if (!kBetween && j0 + kManyTile < j_end) {
+#pragma unroll
+                for (int i = 0; i < NI; ++i) store(i, stage ^ 1, folded_then);
+                if (j0 + 2 * kManyTile < j_end) ahead();
             }
             const unsigned char* kt = smem + stage * 2 * BYTES;
             unsigned char* vt = smem + stage * 2 * BYTES + BYTES;
@@ -810,8 +804,11 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
                         const int row = 32 * x + col;
                         const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + row * (DH * 2) + ((2 * k + half) ^ k_swizzle<DH>(row)) * 16);
                         sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], sc[x], 0, 0, 0);
+                        constexpr int EACH = 2 * KF / NI;
+                        if (kBetween && (x * KF + k) % EACH == EACH - 1) store((x * KF + k) / EACH, stage ^ 1, folded_then);
                     }
                 }
+                if constexpr (kBetween) ahead();
                 const float by = factor(ks * a.scale);
                 float f[4];
                 if constexpr (UNI) {
@@ -930,6 +927,10 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
                         }
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pb[c]), o[d], 0, 0, 0);
                     }
+            } else if constexpr (kBetween) {
+#pragma unroll
+                for (int i = 0; i < NI; ++i) store(i, stage ^ 1, folded_then);
+                ahead();
             }
             ks = ks_then;
             vs = vs_then;
