@@ -93,7 +93,7 @@ __device__ __forceinline__ float max_groups(float x)
 // keys of one key head in turn and join their sums at an item's end (HW = 1), or have a key
 // head each (HW = 4, items then are those of four heads), for heads of 64, whose rows are
 // half a line of memory: read at the same time side by side they come faster (32
-// requests with 2 to 8 tokens each 104 us instead of 148; 64 requests with one 139
+// requests with 2 to 8 tokens each 100 us instead of 148; 64 requests with one 139
 // instead of 211; heads of 128 are no faster so).
 //
 // Bound by the bytes of the cache, in calls of single tokens by the latency of what
