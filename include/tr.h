@@ -527,7 +527,11 @@ tr_status tr_append8(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, 
 /* tr_attend over a cache of 8-bit values (bf16 contexts only); scales are finite and
  * >= 0 where a row sees their tokens.  Keys' scales multiply scores and values'
  * scales weights, in fp32, before these are rounded to bf16, or values' scales the
- * values where that is exact.
+ * values where that is exact.  Values' scales may be as large as fp32 has them; weights
+ * times scales lose what lies below 2^-126, which matters below scales of 2^-100 (powers
+ * of two: 2^-117).  A score is the fp32 sum of q times keys as they are stored, times the
+ * fp32 product of |scale| and the key's scale, at least 2^-126: |q| has to stay below
+ * 2^100 and that product below 2^127.
  * head_dim must be a multiple of 16, and q's, out's and the cache's bases and
  * strides of 16 bytes, else TR_EUNSUPPORTED. */
 tr_status tr_attend8(tr_attn* a, int64_t T, tr_heads q, const tr_cache8* c, const tr_step* s,

@@ -7,8 +7,8 @@
 // An e4m3 value is a bf16 value, so keys and values are widened without loss, two by
 // one instruction, and the products are bf16's.  A key's scale multiplies its scores in
 // fp32, together with the softmax's scale.  A value's goes into that widening where it is
-// a power of two, which is exact, and else multiplies its weights in fp32, before these
-// are rounded to bf16.
+// a power of two, not above kLargeScale, which is exact, and else multiplies its weights in
+// fp32, before these are rounded to bf16.
 #include <algorithm>
 #include <type_traits>
 
@@ -54,12 +54,19 @@ __device__ __forceinline__ int piece8(int row, int piece)
     return piece ^ (DH == 64 ? (row >> 1) & 3 : row & 7);
 }
 
-// Whether a scale is a power of two by which widening is exact: no value leaves bf16's
-// normal range.
+// Sums have up to 2^31 products of a weight, which is 2^8 at most, and a value: finite
+// while values' scales are no larger than this (448 < 2^8.9).  Where a tile has a larger
+// one its rows' weights, and so all that their sums hold, are relative to 2^kRaise times
+// their largest, 2^-40 at most: products with scales of up to 2^128 and their sums are finite
+// then too.  What the sums lose at their small end are values below 2^-70 beside such a scale.
+constexpr float kLargeScale = 0x1p80f, kRaise = 48.f;
+
+// Whether a scale is a power of two by which widening is exact (no value leaves bf16's
+// normal range) and not a large one.
 __device__ __forceinline__ bool is_power(float s)
 {
     const uint32_t w = __float_as_uint(s);
-    return (w & 0x807fffffu) == 0 && w - (10u << 23) < (237u << 23);       // 2^-117 .. 2^119
+    return (w & 0x807fffffu) == 0 && w - (10u << 23) <= (197u << 23);       // 2^-117 .. 2^80
 }
 
 // Queries whose scores are for scale > 0: of -q for scale < 0, of q = 0 for scale 0, NaN
@@ -320,12 +327,13 @@ __global__ __launch_bounds__(kFewThreads, 1) void attend8_few_kernel(Attend8Args
             // Factors of the scores, of sixteen keys each (else in the scores already), and
             // the values' scales: powers of two are for the widening, others for the weights.
             float f[X];
-            bool folded = PG16;
+            bool folded = PG16, large = !PG16 && __any(vs_lane > kLargeScale);
 #pragma unroll
             for (int x = 0; x < X; ++x) {
                 if constexpr (PG16) {
                     f[x] = factor(ks_tile[x] * a.scale);
                     folded = folded && is_power(vs_tile[x]);
+                    large = large || vs_tile[x] > kLargeScale;
                 } else {
                     f[x] = 1.f;
 #pragma unroll
@@ -362,7 +370,7 @@ __global__ __launch_bounds__(kFewThreads, 1) void attend8_few_kernel(Attend8Args
                     const float t = max3(z[0], z[1], max3(z[2], z[3], z[3]));
                     top[i] = max3(top[i], t * f[x], top[i]);
                 }
-                top[i] = max_groups(top[i]);
+                top[i] = max_groups(top[i]) + (large ? kRaise : 0.f);
                 // The maximum that a row's weights are relative to follows only when it is
                 // left behind by 2^8: sums scaled by less than that lose nothing.
                 left[i] = top[i] - m[i] > 8.f;
@@ -841,12 +849,17 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
                     top = max3(top, UNI ? t * f[g] : t, top);
                 }
                 top = max_halves(top);
+                float up = 0.f;
+                if (!folded) {
+                    asm volatile("");      // a branch: append's scales need none of this
+                    up = __any(vs > kLargeScale) ? kRaise : 0.f;
+                }
                 // The maximum that a row's weights are relative to follows only when it is
                 // left behind by 2^8: sums scaled by less than that lose nothing.
-                const bool left = top - m > 8.f;
+                const bool left = top - m > 8.f - up;
                 if (__any(left)) {
-                    const float keep = left ? exp2_(m - top) : 1.f;
-                    m = left ? top : m;
+                    const float keep = left ? exp2_(m - (top + up)) : 1.f;
+                    m = left ? top + up : m;
                     l *= keep;
 #pragma unroll
                     for (int d = 0; d < DT; ++d) o[d] *= keep;
