@@ -37,10 +37,6 @@ def large(t, scale, g, signs):
 @pytest.mark.parametrize("kernel", KERNELS)
 def test_large_values(kernel, dim, page_size, block):
     new, kv, heads, kv_heads, causal = KERNELS[kernel]
-    if kernel in ("in_turn", "items"):
-        if dim == 256:
-            pytest.skip("the same kernel at less cost in the other shapes")
-        heads, kv_heads = heads // kv_heads * 40, 40                 # enough items for an item a workgroup
     g = gen(dim + block)
     step, pages = step_of(new, kv, page_size, g)
     a = tr.Attention(heads, kv_heads, dim, BF)
