@@ -347,7 +347,8 @@ __global__ __launch_bounds__(kFewThreads, 1) void attend8_few_kernel(Attend8Args
             const bool edge = j0 < lo_max || j0 + kTile > hi_min;     // rows past the last are nobody's
             // No branch lies between a matrix instruction and a reader of its result, but for
             // those that skip what all of a tile's rows would do: where several ways lead to a
-            // reader the compiler does not count its wait on all of them.
+            // reader the compiler did not count its wait on all of them
+            // (tests/test_matrix_waits.py walks all of the built kernels' ways).
             u32x4 pb[RT][C];
             float top[RT];
             bool left[RT], any = false;
