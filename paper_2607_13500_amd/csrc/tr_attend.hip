@@ -736,6 +736,7 @@ bool in_halves(const AttendArgs& a)
 template <int DH>
 hipError_t few(const AttendArgs& a, hipStream_t s)
 {
+    static_assert(kPartsFit<DH, kRows, kFewPerCu<DH>>, "the parts' scratch is too small");
     const dim3 grid((unsigned)(kFewPerCu<DH> * a.cus));
     const bool pg16 = in_halves(a);
     auto launch = [&](auto kernel) {
@@ -756,6 +757,7 @@ template <int DH>
 hipError_t many(const AttendArgs& a, hipStream_t s)
 {
     constexpr int NW = kManyWaves<DH>, ROWS = NW * kManyRows;
+    static_assert(kPartsFit<DH, ROWS>, "the parts' scratch is too small");
     // no more items than this, whatever the sequences' lengths
     const int64_t items = ((a.tokens * a.group + ROWS - 1) / ROWS + a.step.seqs) * a.kv_heads;
     auto launch = [&](auto kernel, int64_t groups) {
@@ -776,9 +778,6 @@ hipError_t many(const AttendArgs& a, hipStream_t s)
         return pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, true>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, true>, a.cus);
     return pg16 ? launch(attend_many_kernel<DH, NW, kManyStep, true, false>, a.cus) : launch(attend_many_kernel<DH, NW, kManyStep, false, false>, a.cus);
 }
-
-template <int DH>
-constexpr size_t kGroupFloats = 2 * std::max(kFewPerCu<DH> * kPartFloats<DH, kRows>, kPartFloats<DH, kManyWaves<DH> * kManyRows>);
 
 template <int DH>
 hipError_t attend(const AttendArgs& args, hipStream_t s)
@@ -804,7 +803,7 @@ size_t attend_groups(int cus) { return (size_t)8 * cus; }
 
 size_t attend_part_floats(int dim, int cus)
 {
-    return (size_t)cus * (dim <= 64 ? kGroupFloats<64> : dim <= 128 ? kGroupFloats<128> : kGroupFloats<256>);
+    return (size_t)cus * (dim <= 64 ? kCuFloats<64> : dim <= 128 ? kCuFloats<128> : kCuFloats<256>);
 }
 
 hipError_t launch_attend(const AttendArgs& args, hipStream_t s)

@@ -1044,6 +1044,7 @@ bool in_halves(const Attend8Args& a)
 template <int DH, int HW, int RT>
 hipError_t few(const Attend8Args& args, hipStream_t s)
 {
+    static_assert(kPartsFit<DH, 16 * RT * HW>, "the parts' scratch is too small");
     Attend8Args a = args;
     a.kv_heads /= HW;
     const bool pg16 = in_halves(a);
@@ -1076,6 +1077,7 @@ template <int DH>
 hipError_t many(const Attend8Args& a, hipStream_t s)
 {
     constexpr int NW = kManyWaves<DH>, ROWS = NW * kManyRows;
+    static_assert(kPartsFit<DH, ROWS>, "the parts' scratch is too small");
     // no more items than this, whatever the sequences' lengths
     const int64_t items = ((a.tokens * a.group + ROWS - 1) / ROWS + a.step.seqs) * a.kv_heads;
     auto launch = [&](auto kernel, int64_t groups) {

@@ -295,6 +295,13 @@ __device__ __forceinline__ float2 get2(const float* p)
 template <int DH, int ROWS>
 constexpr int kPartFloats = ROWS * DH + 2 * ROWS;
 
+// Floats of a context's parts for each CU, and whether the two parts of each of PER_CU
+// workgroups fit: each launch that writes parts asserts that its own do.
+template <int DH>
+constexpr int kCuFloats = 2 * kPartFloats<DH, DH == 256 ? 128 : 256>;
+template <int DH, int ROWS, int PER_CU = 1>
+constexpr bool kPartsFit = PER_CU * 2 * kPartFloats<DH, ROWS> <= kCuFloats<DH>;
+
 // One item's parts: `count` of them, this workgroup's is number `mine`, the
 // first is workgroup `owner`'s second.
 struct Parts {
