@@ -146,9 +146,8 @@ def verify_drafts(target: torch.Tensor, ids: torch.Tensor, q_start: torch.Tensor
         if columns != vocab:
             raise ValueError("draft must have target's %d columns (got %d)" % (vocab, columns))
     lib = _lib.load()
-    # the scratch first, whose address has to be of 16 bytes
-    scratch, said, accepted, change = _empty((lib.tr_verify_scratch(seqs) // 4 + seqs * (width + 2),), _I32, target.device, stream) \
-        .unsafe_split_with_sizes([lib.tr_verify_scratch(seqs) // 4, seqs * width, seqs, seqs])
+    said, accepted, change = _empty((seqs * (width + 2),), _I32, target.device, stream).unsafe_split_with_sizes([seqs * width, seqs, seqs])
+    scratch = _empty((lib.tr_verify_scratch(seqs),), torch.uint8, target.device, stream)    # 4 KB a sequence, not kept with the results
     _run(lib.tr_verify_drafts, "tr_verify_drafts", index, stream, tokens, vocab, _DTYPES[dtype], p, ld, q, ld_draft,
          _vector("ids", ids, index, _I32, tokens), seqs, _vector("q_start", q_start, index, _I32, seqs + 1),
          _vector("accept", accept, index, _F32, tokens), _vector("draw", draw, index, _F32, seqs), width,
