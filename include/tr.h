@@ -557,8 +557,9 @@ typedef struct {
  *               and are not taken in the same call
  *   q_start[b]  = sum of max(change, 0) over the sequences before b    [seqs + 1]
  *   slots, pos  for each of the rows packed rows: page * page_size + row in the cache
- *               (int64) and the place in the sequence (int32); rows that belong to no
- *               sequence get -1 and 0.  Either may be NULL.
+ *               (int64) and the place in the sequence (int32), which is its position
+ *               where there is one axis and each token counts as one; rows that belong
+ *               to no sequence get -1 and 0.  Either may be NULL.
  *   short_of    0; or the number of pages that the pool lacks; or 2^31 - 1 where a
  *               sequence outgrows its row of the table, or the new tokens the rows.
  *               Then nothing else changes: kv_out and state_out are kv_len and

@@ -31,7 +31,7 @@ class PagePool(NamedTuple):
 class PageUpdate(NamedTuple):
     step: Step                     # q_start, the new lengths, the table
     slots: torch.Tensor            # int64 [rows] page * page_size + row of each new token, -1 behind them
-    pos: torch.Tensor              # int32 [rows] its place in its sequence, 0 behind them
+    pos: torch.Tensor              # int32 [rows] its place in its sequence (tokens before it), 0 behind them
     pool: PagePool                 # the ring and its new state
     short: torch.Tensor            # int32 [1]: 0, or the pages that are lacking (then nothing has changed)
 
@@ -85,6 +85,11 @@ def update_pages(change: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor
     pool lacks pages, a sequence outgrows its row of the table or the new tokens the
     rows, nothing changes, no row belongs to any sequence, and `short` is the number of
     lacking pages, in the last two cases 2^31 - 1.
+
+    `pos` is a token's position in a context of one axis whose tokens count as one each;
+    append takes it as it is then.  Contexts of several axes take int32 [axes, rows], and
+    text behind an image's kept tokens, which have their grid's positions, is a number
+    of positions ahead of its places that the caller knows for each sequence.
 
     in_place: the new lengths and the pool's new state are written to kv_len and
     pool.state themselves, as a recorded graph that is replayed needs it.
