@@ -587,7 +587,7 @@ tr_status tr_update_pages(int32_t seqs, const int32_t* change, const int32_t* kv
  *   weights up to it exceeds draw[b] times their sum; 0 where all are 0.
  *   tokens[b]   = the accepted drafts, t, then -1                [seqs, width]
  *   change[b]   = accepted[b] minus the sequence's drafts: what its length changes by
- *                 (tr_update_pages)
+ *                 (tr_update_pages, in a call of its own: one gives up tokens or adds some)
  * A sequence of no rows has tokens of -1 and 0s.  Probabilities need not be normed;
  * NaN, negative and infinite ones count as 0.  accept and draw lie in [0, 1).  Drafts
  * outside [0, vocab) are rejected.  Products, differences and sums are in 64 bits.

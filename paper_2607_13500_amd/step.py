@@ -7,7 +7,8 @@ include/tr.h):
                    token drawn behind them, from given random numbers.
 
 A decoding step with drafts is update_pages, the model (Attention.append and attend
-in each layer), verify_drafts, and its `change` goes into the next update_pages.
+in each layer), verify_drafts, and update_pages with its `change`, by which the rejected
+drafts leave before the next step adds tokens.
 """
 from __future__ import annotations
 
@@ -39,7 +40,7 @@ class PageUpdate(NamedTuple):
 class Verified(NamedTuple):
     tokens: torch.Tensor           # int32 [seqs, width]: accepted drafts, the drawn token, then -1
     accepted: torch.Tensor         # int32 [seqs] accepted drafts
-    change: torch.Tensor           # int32 [seqs] accepted minus drafted: what the sequence's length changes by
+    change: torch.Tensor           # int32 [seqs] accepted minus drafted: what the sequence's length changes by, for update_pages
 
 
 # Small calls are bound by this module's own work (64 requests' tables: 11 us a call
@@ -85,6 +86,10 @@ def update_pages(change: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor
     pool lacks pages, a sequence outgrows its row of the table or the new tokens the
     rows, nothing changes, no row belongs to any sequence, and `short` is the number of
     lacking pages, in the last two cases 2^31 - 1.
+
+    A sequence gains or loses tokens in one call, not both: what Verified.change takes
+    away goes in a call of its own (of no rows) before the one that adds the next tokens.
+    The sum of the two in one call would add too few rows, at later places.
 
     `pos` is a token's position in a context of one axis whose tokens count as one each;
     append takes it as it is then.  Contexts of several axes take int32 [axes, rows], and
