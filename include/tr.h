@@ -481,8 +481,8 @@ tr_status tr_append(tr_attn* a, int64_t T, tr_heads q, tr_heads k, tr_heads v, c
  *   j <= p with `causal`, and of those j > p - window with window > 0 (window
  *   needs causal); all kv_len[b] tokens otherwise.
  * A row that sees no token, or whose scores are all -inf, is 0, its lse -inf.
- * Scores and sums are fp32; the weights are rounded to bf16 for their product
- * with v.  Elements that a row does not see do not change it, NaN and infinite
+ * Scores and sums are fp32 (sums hold weights of up to 2^8, and are finite for values
+ * below 2^80); the weights are rounded to bf16 for their product with v.  Elements that a row does not see do not change it, NaN and infinite
  * ones included.
  *   lse: device float [T, heads] natural logarithm of the softmax's sum, or NULL
  * head_dim must be a multiple of 8, and q's, out's and the cache's bases and
@@ -595,7 +595,8 @@ tr_status tr_update_pages(int32_t seqs, const int32_t* change, const int32_t* kv
  *   ids            device int32 [T]; accept device float [T]; draw device float [seqs]
  *   scratch        device, tr_verify_scratch(seqs) bytes, 16-byte aligned, of one
  *                  call at a time; its contents mean nothing before and after
- * q_start is not checked by the host: rows outside [0, T) are never read. */
+ * q_start is not checked by the host: rows outside [0, T) are never read.  What is
+ * written shares memory with nothing else. */
 size_t tr_verify_scratch(int32_t seqs);
 tr_status tr_verify_drafts(int64_t T, int32_t vocab, int32_t dtype, const void* target, int64_t ld_target,
                            const void* draft, int64_t ld_draft, const int32_t* ids, int32_t seqs,

@@ -67,7 +67,8 @@ class KVCache8(NamedTuple):
     """A paged cache in 8 bits: k and v float8_e4m3fn as in KVCache, and float32 scales
     [pages, blocks, kv_heads] of any (the same) strides: row r of page g of head h
     stands for k[g, r, h] * k_scale[g, r // (page_size // blocks), h].  append makes
-    the scales powers of two; attend takes any that are finite and >= 0."""
+    the scales powers of two; attend takes any that are finite and >= 0 (how far is said
+    in include/tr.h, at tr_attend8)."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor

@@ -113,7 +113,8 @@ template <int DH>
 constexpr int kFewTile = DH == 64 ? 64 : 32;
 
 // PG16: pages and blocks of whole halves of a tile (multiples of 16 tokens, pages below
-// 2 GB), so that a half's page and scales are the wavefront's.  FULL: head_dim is DH.
+// 2 GB), so that a half's page and scales are the wavefront's (pages of 40 in blocks of 8:
+// the 64 requests 118 us, the 32 119).  FULL: head_dim is DH.
 // kv_heads counts groups of HW heads here.
 template <int DH, int HW, int RT, bool PG16, bool FULL>
 __global__ __launch_bounds__(kFewThreads, 1) void attend8_few_kernel(Attend8Args a)
@@ -627,13 +628,15 @@ __global__ __launch_bounds__(kFewThreads, 1) void attend8_few_kernel(Attend8Args
 // one the bytes are in registers, of the one after it on their way there.  Widening in
 // the stage is shared by all wavefronts; from there on a tile is the bf16 kernel's, whose
 // bounds (matrix instructions and the softmax between them) are this one's (a prompt of
-// 18432 tokens, 32 query and 8 key heads of 128: 2.86 ms, 972 TFLOP/s; the kernel for
+// 18432 tokens, 32 query and 8 key heads of 128: 2.82-2.91 ms, 955-985 TFLOP/s; the kernel for
 // few rows, 16 rows an item: 19.2 ms).
 //
 // Values' scales that are powers of two go into the widening, which is exact, else
 // they multiply the weights.  Keys' scales multiply scores, in the multiply-add that
 // takes the maximum off.
-// UNI: pages and blocks of whole 16 tokens, so that a scale is that of 16 keys.
+// UNI: pages and blocks of whole 16 tokens, so that a scale is that of 16 keys; else each
+// score is multiplied by its own key's (pages of 40 in blocks of 8: the prompt 4.20 ms, chunks
+// of 8 requests 774 us and not 533).
 template <int DH, int NW, int STEP, bool UNI, bool FULL>
 __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kernel(Attend8Args a)
 {
@@ -643,9 +646,9 @@ __global__ __launch_bounds__(NW * 64, DH == 256 ? 1 : 2) void attend8_many_kerne
     constexpr int PIECES = DH / 16, NP = kManyTile * PIECES;   // pieces of a row and of a tile, 16 bytes each
     constexpr int NI = 2 * NP / T;                          // of a thread, keys' before values'
     // Items by themselves widen the next tile's pieces between the first product's
-    // instructions (a prompt of 8192 tokens, 8 heads of 64: 429 us, before it 458; 4 of 256:
-    // 2922 and 3010; 18432 tokens, 8 of 128: 1 %).  Shares widen them before it: between,
-    // chunks of 8 requests with 4 heads of 128 took 550 us and not 530.
+    // instructions (a prompt of 8192 tokens, 8 heads of 64: 435 us, before it 442; 4 of 256:
+    // 2936 and 3276; 18432 tokens, 8 of 128: 2835 and 2890).  Shares widen them before it:
+    // between, chunks of 8 requests with 4 heads of 128 take 546 us and not 533.
     constexpr bool kBetween = STEP == 0;
     __shared__ __align__(16) unsigned char smem[4 * BYTES]; // stage 0: K, V; stage 1: K, V
     __shared__ int flag;
