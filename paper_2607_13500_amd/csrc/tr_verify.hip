@@ -370,7 +370,7 @@ __global__ __launch_bounds__(64) void verify_draw_kernel(VerifyArgs a)
 
 // Rows of at most kOneWords: a workgroup a sequence, in one launch.  Each wavefront has
 // one slice, of whose sums all wavefronts see where the mark falls.  Bound by one CU's
-// 64-bit additions (a call of 1 to 64 sequences and a draft's words, on one box: 32000
+// 64-bit additions (a call of 1 to 64 sequences and a draft's words: 32000
 // fp32 or bf16 words 13.3 us, 16.0 in two launches; 40000 words 15 to 18.4, and 16.0; 64000
 // fp32 words 14.2 with one sequence, 16.9 with 16, 19.5 with 64, and 15.8.  256 sequences of
 // 40000 words: 24.1 and 23.5 fp32, 19.1 and 33.8 bf16).
